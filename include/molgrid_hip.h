@@ -293,6 +293,92 @@ int mg_backward_vector_f64(const mg_gridmaker *gm, int B, int N, int T,
                            float *grad_coords, float *grad_weights,
                            void *workspace, size_t workspace_bytes, void *stream);
 
+/*
+ * Microscaled formats: numbers in 8 or 4 bits.  What a network keeps for its
+ * backward pass is kept in 8 bits and its weight gradients are formed from the
+ * codes; linear maps of atom features (types learned from features) run in 4
+ * bits where no gradient is wanted.
+ *
+ * A matrix of rows x cols numbers is cut into blocks of 32 along each row (the
+ * last one filled up with zeros); a block shares a power of two, as in the OCP
+ * Microscaling Formats Specification v1.0.  With a the block's largest
+ * magnitude, k = floor(log2 a), one more where a / 2^k >= over,
+ *     scale byte S = clamp(k - emax + 127, 0, 254)
+ *     element      = x * 2^(127-S) to the nearest, ties to even, saturating
+ *     value        = element * 2^(S-127)
+ * A block that holds an infinity or a NaN has S = 255 and codes 0, and every
+ * value of it is NaN.
+ *     MG_MX_INT8   whole numbers -127..127       emax 6   over 255/128
+ *     MG_MX_E4M3   4 significant bits, +-448     emax 8   over 29/16
+ *     MG_MX_E2M1   0 .5 1 1.5 2 3 4 6 (4 bits)   emax 2   over 7/4
+ * so a value is off by at most half a step of its element: int8 2^(k-7), e4m3
+ * 2^-4 of itself (or 2^(k-18)), e2m1 2^-2 of itself (or 2^(k-4)).
+ * Layout, with blocks = ceil(cols/32):
+ *     codes   [rows][32*blocks] bytes, MG_MX_E2M1 [rows][16*blocks], the even
+ *             element in the low four bits; 16-byte aligned
+ *     scales  [rows][blocks rounded up to a multiple of 4] bytes; 4-byte
+ *             aligned; the filling is written as zeros
+ * Plain numbers are MG_F32, MG_F16 or MG_BF16, elements of a row next to each
+ * other and rows row_stride elements apart (>= cols; not looked at where there
+ * is one row), aligned to their own size.  Limits: rows <= 2^31-1, rows times the
+ * scale row < 2^31 (else MG_ESHAPE).
+ */
+enum { MG_F32 = 0, MG_F16 = 1, MG_BF16 = 2 };
+enum { MG_MX_INT8 = 0, MG_MX_E4M3 = 1, MG_MX_E2M1 = 2 };
+
+/* Numbers into codes; every byte of codes and scales is written. */
+int mg_mx_pack(int format, int dtype, int64_t rows, int64_t cols, const void *x,
+               int64_t row_stride, uint8_t *codes, uint8_t *scales, void *stream);
+
+/*
+ * Codes into numbers, rounded once to dtype (exact but for MG_F16 outside its
+ * range); a finite value past the largest finite number of dtype becomes that
+ * number.  Nothing between a row's end and the next row is written.
+ */
+int mg_mx_unpack(int format, int dtype, int64_t rows, int64_t cols, const uint8_t *codes,
+                 const uint8_t *scales, void *x, int64_t row_stride, void *stream);
+
+/*
+ * Weight gradient of y = x W^T + b over the atoms of a batch, from the 8-bit
+ * codes of x (MG_MX_INT8 or MG_MX_E4M3, B*N rows of E):
+ *     grad_weight[t][e] = sum_{b, a < natoms[b]} grad[b][a][t] * x[b][a][e]
+ *     grad_bias[t]      = sum_{b, a < natoms[b]} grad[b][a][t]
+ * grad: B*N rows of T numbers, grad_stride >= T elements apart; grad_weight
+ * [T][E] and grad_bias [T] (may be NULL) float, written.  natoms [B] or NULL
+ * (all N): rows past it count for nothing, whatever they hold.  Codes and
+ * gradients enter exactly (blocks of magnitudes below 2^-120 as zero), sums
+ * are float in a fixed order.  B*N < 2^31-255, T <= 65535, E <= 2^20 (else
+ * MG_ESHAPE).  The workspace (32-byte aligned) is scratch.
+ */
+int mg_mx8_weight_gradient_workspace(int B, int N, int T, int E, size_t *bytes);
+int mg_mx8_weight_gradient(int format, int dtype, int B, int N, int T, int E, const void *grad,
+                           int64_t grad_stride, const uint8_t *codes, const uint8_t *scales,
+                           const int32_t *natoms, float *grad_weight, float *grad_bias,
+                           void *workspace, size_t workspace_bytes, void *stream);
+
+/*
+ * Product of two matrices in MG_MX_E2M1:
+ *     out[m][n] = sum_k a[m][k] * b[n][k] + bias[n]
+ * a [M] rows, b [N] rows of K; out [M] rows of N numbers of dtype, out_stride
+ * >= N elements apart, nothing between them written; bias [N] float or NULL.
+ * Products are exact, sums are float, rounded once to dtype.  A NaN block makes
+ * its row (of a) or column (of b) NaN.  M <= 2^30, N <= 2^20-16, K <= 2^24.
+ */
+int mg_mx4_product(int dtype, int M, int N, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                   const uint8_t *b_codes, const uint8_t *b_scales, const float *bias, void *out,
+                   int64_t out_stride, void *stream);
+
+/*
+ * mg_mx4_product with a in plain numbers of dtype (rows x_stride >= K elements
+ * apart), taken to MG_MX_E2M1 by the call exactly as mg_mx_pack does.  One
+ * launch without a workspace where rows or columns are few
+ * (mg_mx4_linear_workspace gives 0), else pack and product.
+ */
+int mg_mx4_linear_workspace(int M, int N, int K, size_t *bytes);
+int mg_mx4_linear(int dtype, int M, int N, int K, const void *x, int64_t x_stride,
+                  const uint8_t *w_codes, const uint8_t *w_scales, const float *bias, void *out,
+                  int64_t out_stride, void *workspace, size_t workspace_bytes, void *stream);
+
 /* Text for an MG_* code (static storage). */
 const char *mg_strerror(int code);
 

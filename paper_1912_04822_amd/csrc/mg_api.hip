@@ -8,6 +8,7 @@
 #include <new>
 
 #include "mg_common.h"
+#include "mg_mx_ops.h"
 
 struct mg_gridmaker {
     mg::GridSpec gs;
@@ -516,17 +517,148 @@ int mg_backward_vector_f64(const mg_gridmaker *gm, int B, int N, int T, const fl
                          workspace_bytes, stream);
 }
 
+// ---- microscaled formats ----
+
+static bool mx_type(int dtype) { return dtype == MG_F32 || dtype == MG_F16 || dtype == MG_BF16; }
+
+static bool misaligned(const void *p, unsigned bytes) { return p && ((uintptr_t)p & (bytes - 1)) != 0; }
+
+static bool misaligned_number(const void *p, int dtype) { return misaligned(p, dtype == MG_F32 ? 4 : 2); }
+
+static bool misaligned_codes(const void *codes, const void *scales)
+{
+    return misaligned(codes, 16) || misaligned(scales, 4);
+}
+
+// rows x cols numbers, row_stride apart: the blocks of the scale rows are counted in 31 bits
+static int check_mx_rows(int64_t rows, int64_t cols, int64_t row_stride)
+{
+    if (rows < 1 || cols < 1 || cols > ((int64_t)1 << 36) || rows > 0x7fffffff) return MG_ESHAPE;
+    if (rows * mg::mx_scale_pitch(cols) > 0x7fffffffLL) return MG_ESHAPE;
+    if (rows > 1 && (row_stride < cols || row_stride > ((int64_t)1 << 40))) return MG_ESHAPE;
+    return MG_OK;
+}
+
+int mg_mx_pack(int format, int dtype, int64_t rows, int64_t cols, const void *x, int64_t row_stride,
+               uint8_t *codes, uint8_t *scales, void *stream)
+{
+    if (!x || !codes || !scales) return MG_ENULL;
+    if (format < MG_MX_INT8 || format > MG_MX_E2M1 || !mx_type(dtype)) return MG_EPARAM;
+    const int rc = check_mx_rows(rows, cols, row_stride);
+    if (rc != MG_OK) return rc;
+    if (misaligned_number(x, dtype) || misaligned_codes(codes, scales)) return MG_EALIGN;
+    return hip_status(mg::launch_mx_pack((mg::Mx)format, (mg::Num)dtype, rows, cols, x, row_stride, codes,
+                                         scales, (hipStream_t)stream));
+}
+
+int mg_mx_unpack(int format, int dtype, int64_t rows, int64_t cols, const uint8_t *codes,
+                 const uint8_t *scales, void *x, int64_t row_stride, void *stream)
+{
+    if (!x || !codes || !scales) return MG_ENULL;
+    if (format < MG_MX_INT8 || format > MG_MX_E2M1 || !mx_type(dtype)) return MG_EPARAM;
+    const int rc = check_mx_rows(rows, cols, row_stride);
+    if (rc != MG_OK) return rc;
+    if (misaligned_number(x, dtype) || misaligned_codes(codes, scales)) return MG_EALIGN;
+    return hip_status(mg::launch_mx_unpack((mg::Mx)format, (mg::Num)dtype, rows, cols, codes, scales, x,
+                                           row_stride, (hipStream_t)stream));
+}
+
+static int check_mx_gradient(int B, int N, int T, int E)
+{
+    if (B < 1 || N < 1 || T < 1 || E < 1 || T > 65535 || E > (1 << 20)) return MG_ESHAPE;
+    if ((int64_t)B * N > 0x7fffff00LL) return MG_ESHAPE;
+    return MG_OK;
+}
+
+int mg_mx8_weight_gradient_workspace(int B, int N, int T, int E, size_t *bytes)
+{
+    if (!bytes) return MG_ENULL;
+    const int rc = check_mx_gradient(B, N, T, E);
+    if (rc != MG_OK) return rc;
+    *bytes = mg::mx_gradient_workspace((int64_t)B * N, T, E);
+    return MG_OK;
+}
+
+int mg_mx8_weight_gradient(int format, int dtype, int B, int N, int T, int E, const void *grad,
+                           int64_t grad_stride, const uint8_t *codes, const uint8_t *scales,
+                           const int32_t *natoms, float *grad_weight, float *grad_bias, void *workspace,
+                           size_t workspace_bytes, void *stream)
+{
+    if (!grad || !codes || !scales || !grad_weight) return MG_ENULL;
+    if ((format != MG_MX_INT8 && format != MG_MX_E4M3) || !mx_type(dtype)) return MG_EPARAM;
+    const int rc = check_mx_gradient(B, N, T, E);
+    if (rc != MG_OK) return rc;
+    if (grad_stride < T || grad_stride > ((int64_t)1 << 40)) return MG_ESHAPE;
+    if (misaligned_number(grad, dtype) || misaligned_codes(codes, scales) || misaligned4(natoms) ||
+        misaligned4(grad_weight) || misaligned4(grad_bias))
+        return MG_EALIGN;
+    const size_t need = mg::mx_gradient_workspace((int64_t)B * N, T, E);
+    if (need > 0 && (!workspace || misaligned(workspace, 32) || workspace_bytes < need)) return MG_EWORKSPACE;
+    return hip_status(mg::launch_mx_gradient((mg::Mx)format, (mg::Num)dtype, B, N, T, E, grad, grad_stride,
+                                             codes, scales, natoms, grad_weight, grad_bias, workspace,
+                                             (hipStream_t)stream));
+}
+
+static int check_mx_product(int M, int N, int K, int64_t out_stride)
+{
+    if (M < 1 || N < 1 || K < 1 || M > (1 << 30) || N > (1 << 20) - 16 || K > (1 << 24)) return MG_ESHAPE;
+    if (out_stride < N || out_stride > ((int64_t)1 << 40)) return MG_ESHAPE;
+    return MG_OK;
+}
+
+int mg_mx4_product(int dtype, int M, int N, int K, const uint8_t *a_codes, const uint8_t *a_scales,
+                   const uint8_t *b_codes, const uint8_t *b_scales, const float *bias, void *out,
+                   int64_t out_stride, void *stream)
+{
+    if (!a_codes || !a_scales || !b_codes || !b_scales || !out) return MG_ENULL;
+    if (!mx_type(dtype)) return MG_EPARAM;
+    const int rc = check_mx_product(M, N, K, out_stride);
+    if (rc != MG_OK) return rc;
+    if (misaligned_codes(a_codes, a_scales) || misaligned_codes(b_codes, b_scales) || misaligned4(bias) ||
+        misaligned_number(out, dtype))
+        return MG_EALIGN;
+    return hip_status(mg::launch_mx4_product((mg::Num)dtype, M, N, K, a_codes, a_scales, b_codes, b_scales, bias,
+                                             out, out_stride, (hipStream_t)stream));
+}
+
+int mg_mx4_linear_workspace(int M, int N, int K, size_t *bytes)
+{
+    if (!bytes) return MG_ENULL;
+    const int rc = check_mx_product(M, N, K, N);
+    if (rc != MG_OK) return rc;
+    *bytes = mg::mx4_linear_workspace(M, N, K);
+    return MG_OK;
+}
+
+int mg_mx4_linear(int dtype, int M, int N, int K, const void *x, int64_t x_stride, const uint8_t *w_codes,
+                  const uint8_t *w_scales, const float *bias, void *out, int64_t out_stride, void *workspace,
+                  size_t workspace_bytes, void *stream)
+{
+    if (!x || !w_codes || !w_scales || !out) return MG_ENULL;
+    if (!mx_type(dtype)) return MG_EPARAM;
+    int rc = check_mx_product(M, N, K, out_stride);
+    if (rc == MG_OK) rc = check_mx_rows(M, K, x_stride);
+    if (rc != MG_OK) return rc;
+    if (misaligned_number(x, dtype) || misaligned_codes(w_codes, w_scales) || misaligned4(bias) ||
+        misaligned_number(out, dtype))
+        return MG_EALIGN;
+    const size_t need = mg::mx4_linear_workspace(M, N, K);
+    if (need > 0 && (!workspace || misaligned(workspace, 32) || workspace_bytes < need)) return MG_EWORKSPACE;
+    return hip_status(mg::launch_mx4_linear((mg::Num)dtype, M, N, K, x, x_stride, w_codes, w_scales, bias, out,
+                                            out_stride, workspace, (hipStream_t)stream));
+}
+
 const char *mg_strerror(int code)
 {
     switch (code) {
     case MG_OK: return "ok";
     case MG_ENULL: return "a required pointer is NULL";
     case MG_ESHAPE: return "bad shape: B, N, T must be >= 1, B <= 65535, 1 <= D <= 1024, sizes must fit";
-    case MG_EPARAM: return "bad parameter: resolution, radius_scale and gaussian_radius_multiple must be finite and positive";
-    case MG_EWORKSPACE: return "workspace is NULL, not 32-byte aligned, or smaller than mg_workspace_bytes";
+    case MG_EPARAM: return "bad parameter: resolution, radius_scale and gaussian_radius_multiple must be finite and positive, format and dtype known";
+    case MG_EWORKSPACE: return "workspace is NULL, not 32-byte aligned, or smaller than the call needs (mg_workspace_bytes, mg_*_workspace)";
     case MG_EHIP: return "the HIP runtime refused a launch (mg_last_hip_error has the hipError_t)";
     case MG_EMODE: return "call not defined for this GridMaker (binary backward, or vector types without radius_type_indexed)";
-    case MG_EALIGN: return "an array argument is not 4-byte aligned";
+    case MG_EALIGN: return "an array argument is not aligned to its elements (codes: 16 bytes, scales: 4)";
     case MG_ENOMEM: return "out of host memory";
     default: return "unknown error code";
     }

@@ -26,6 +26,8 @@ EXPORTS = [
     "mg_prepare", "mg_forward_index_prepared", "mg_forward_vector_prepared",
     "mg_backward_index_prepared", "mg_backward_vector_prepared",
     "mg_set_option", "mg_time_next_kernel",
+    "mg_mx_pack", "mg_mx_unpack", "mg_mx8_weight_gradient", "mg_mx8_weight_gradient_workspace",
+    "mg_mx4_product", "mg_mx4_linear", "mg_mx4_linear_workspace",
 ]
 
 _lib: Optional[ctypes.CDLL] = None
@@ -95,6 +97,17 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
         L.mg_backward_index_prepared.argtypes = [vp, ci, ci, ci, vp, vp, vp, sz, vp]
         L.mg_backward_vector_prepared.restype = ci
         L.mg_backward_vector_prepared.argtypes = [vp, ci, ci, ci, vp, vp, vp, vp, vp, vp, sz, vp]
+        i64 = ctypes.c_int64
+        for name, args in (
+                ("mg_mx_pack", [ci, ci, i64, i64, vp, i64, vp, vp, vp]),
+                ("mg_mx_unpack", [ci, ci, i64, i64, vp, vp, vp, i64, vp]),
+                ("mg_mx8_weight_gradient_workspace", [ci] * 4 + [ctypes.POINTER(sz)]),
+                ("mg_mx8_weight_gradient", [ci] * 6 + [vp, i64] + [vp] * 6 + [sz, vp]),
+                ("mg_mx4_product", [ci] * 4 + [vp] * 6 + [i64, vp]),
+                ("mg_mx4_linear_workspace", [ci] * 3 + [ctypes.POINTER(sz)]),
+                ("mg_mx4_linear", [ci] * 4 + [vp, i64] + [vp] * 4 + [i64, vp, sz, vp])):
+            getattr(L, name).restype = ci
+            getattr(L, name).argtypes = args
         L.mg_strerror.restype = ctypes.c_char_p
         L.mg_strerror.argtypes = [ci]
         L.mg_last_hip_error.restype = ci
@@ -437,3 +450,230 @@ class GridMaker:
         if rc != MG_OK:
             raise MolgridError(rc, "mg_backward_vector_prepared")
         return grad_coords, grad_weights
+
+
+# ---- microscaled formats: numbers in 8 or 4 bits ----
+
+MX_FORMATS = {"int8": 0, "e4m3": 1, "e2m1": 2}          # MG_MX_INT8, MG_MX_E4M3, MG_MX_E2M1
+_NUMBERS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # MG_F32, MG_F16, MG_BF16
+
+
+class MXTensor:
+    """A tensor in a microscaled format: ``codes`` and ``scales`` (uint8 device tensors laid out as
+    include/molgrid_hip.h says, one row for every index but the last), the ``shape`` it stands for,
+    the ``format`` ("int8", "e4m3" or "e2m1") and the ``dtype`` ``mg_mx_unpack`` gives back."""
+
+    __slots__ = ("codes", "scales", "shape", "format", "dtype")
+
+    def __init__(self, codes, scales, shape, format, dtype=torch.float32):
+        self.codes, self.scales, self.shape = codes, scales, tuple(shape)
+        self.format, self.dtype = format, dtype
+
+    @property
+    def rows(self):
+        n = 1
+        for d in self.shape[:-1]:
+            n *= d
+        return n
+
+    def __repr__(self):
+        return "MXTensor(%s, %s)" % (self.format, list(self.shape))
+
+
+def _mx_layout(shape, format):
+    """(rows, columns), shapes of codes and scales."""
+    if format not in MX_FORMATS:
+        raise ValueError("format must be one of %s, got %r" % (", ".join(MX_FORMATS), format))
+    if len(shape) == 0:
+        raise ValueError("a tensor in a microscaled format has at least one dimension")
+    rows, cols = 1, shape[-1]
+    for d in shape[:-1]:
+        rows *= d
+    blocks = (cols + 31) // 32
+    return rows, cols, (rows, blocks * (16 if format == "e2m1" else 32)), (rows, (blocks + 3) // 4 * 4)
+
+
+def _mx_pointers(t, name, formats, device):
+    """Checks an MXTensor; (rows, columns, codes, scales)."""
+    if not isinstance(t, MXTensor):
+        raise TypeError("%s must be an MXTensor, got %s" % (name, type(t).__name__))
+    if t.format not in formats:
+        raise ValueError("%s must be in %s, got %s" % (name, " or ".join(formats), t.format))
+    rows, cols, cshape, sshape = _mx_layout(t.shape, t.format)
+    codes = _ptr(t.codes, torch.uint8, name + ".codes", cshape)
+    scales = _ptr(t.scales, torch.uint8, name + ".scales", sshape)
+    _same_device(device, **{name + ".codes": t.codes, name + ".scales": t.scales})
+    return rows, cols, codes, scales
+
+
+def _same_device(device, **tensors):
+    for name, t in tensors.items():
+        if t is not None and t.device != device:
+            raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+
+
+def _number(dtype, name):
+    code = _NUMBERS.get(dtype)
+    if code is None:
+        raise TypeError("%s must be float32, float16 or bfloat16, got %s" % (name, dtype))
+    return code
+
+
+def _row_stride(t, name):
+    """Elements from row to row of a tensor whose rows (last dimension) are equally far apart."""
+    if not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    if t.is_contiguous():
+        return t.shape[-1]
+    if t.shape[-1] > 1 and t.stride(-1) != 1:
+        raise ValueError("the last dimension of %s must be contiguous" % name)
+    step = None
+    for d in range(t.dim() - 2, -1, -1):        # the innermost dimension that has a step fixes it
+        if t.shape[d] == 1:
+            continue
+        if step is None:
+            step = unit = t.stride(d)
+        elif t.stride(d) != unit:
+            raise ValueError("the rows of %s must be equally far apart" % name)
+        unit *= t.shape[d]
+    if step is None:
+        return t.shape[-1]
+    if step < t.shape[-1]:
+        raise ValueError("the rows of %s overlap" % name)
+    return step
+
+
+def _on(device):
+    """Launches go to the tensors' device, whichever is current."""
+    return torch.cuda.device(device)
+
+
+def _current(device):
+    return device.index == torch.cuda.current_device()
+
+
+def _launch(name, device, *args):
+    """One library call on the device's current stream."""
+    fn = getattr(lib(), name)
+    if _current(device):
+        rc = fn(*args, _stream())
+    else:
+        with _on(device):
+            rc = fn(*args, _stream())
+    if rc != MG_OK:
+        raise MolgridError(rc, name)
+
+
+def _scratch(name, device, *sizes):
+    """The workspace a call of these sizes needs (bytes from ``name``), or None."""
+    n = ctypes.c_size_t()
+    rc = getattr(lib(), name)(*sizes, ctypes.byref(n))
+    if rc != MG_OK:
+        raise MolgridError(rc, name)
+    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+
+
+def mg_mx_pack(x, format="int8", out: Optional[MXTensor] = None) -> MXTensor:
+    """``x`` (float32, float16 or bfloat16; rows along the last dimension, equally far apart) in
+    blocks of 32 numbers that share a power of two."""
+    rows, cols, cshape, sshape = _mx_layout(x.shape, format)
+    dtype, stride = _number(x.dtype, "x"), _row_stride(x, "x")
+    if out is None:
+        out = MXTensor(torch.empty(cshape, dtype=torch.uint8, device=x.device),
+                       torch.empty(sshape, dtype=torch.uint8, device=x.device), x.shape, format, x.dtype)
+        codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
+    else:
+        if out.shape != tuple(x.shape):
+            raise ValueError("out must have shape %s, got %s" % (tuple(x.shape), out.shape))
+        _, _, codes, scales = _mx_pointers(out, "out", (format,), x.device)
+        out.dtype = x.dtype
+    _launch("mg_mx_pack", x.device, MX_FORMATS[format], dtype, rows, cols, x.data_ptr(), stride, codes, scales)
+    return out
+
+
+def mg_mx_unpack(packed: MXTensor, dtype=None, out=None):
+    """The numbers ``packed`` stands for, as a tensor of its shape (``dtype``: default its own)."""
+    device = packed.codes.device
+    rows, cols, codes, scales = _mx_pointers(packed, "packed", tuple(MX_FORMATS), device)
+    if out is None:
+        out = torch.empty(packed.shape, dtype=dtype or packed.dtype, device=device)
+    elif tuple(out.shape) != packed.shape:
+        raise ValueError("out must have shape %s, got %s" % (packed.shape, tuple(out.shape)))
+    number, stride = _number(out.dtype, "out"), _row_stride(out, "out")
+    _same_device(device, out=out)
+    _launch("mg_mx_unpack", device, MX_FORMATS[packed.format], number, rows, cols, codes, scales, out.data_ptr(),
+            stride)
+    return out
+
+
+def mg_mx8_weight_gradient(grad, packed: MXTensor, natoms=None, grad_weight=None, grad_bias=None):
+    """(``grad_weight`` [T,E], ``grad_bias`` [T]) in float32 of y = x W^T + b, from ``grad`` [...,T]
+    on y and the 8-bit codes of x [...,E].  ``natoms`` [B] (x of shape [B,N,E]): atoms past it
+    count for nothing, whatever their rows hold."""
+    device = grad.device
+    rows, E, codes, scales = _mx_pointers(packed, "packed", ("int8", "e4m3"), device)
+    T = grad.shape[-1]
+    if tuple(grad.shape[:-1]) != packed.shape[:-1]:
+        raise ValueError("grad must have shape %s, got %s" % (packed.shape[:-1] + (T,), tuple(grad.shape)))
+    B, N = (packed.shape[0], packed.shape[1]) if len(packed.shape) == 3 else (1, rows)
+    if natoms is not None and len(packed.shape) != 3:
+        raise ValueError("natoms needs x of shape [B,N,E], got %s" % (packed.shape,))
+    number, stride = _number(grad.dtype, "grad"), _row_stride(grad, "grad")
+    if grad_weight is None:
+        grad_weight = torch.empty((T, E), dtype=torch.float32, device=device)
+    if grad_bias is None:
+        grad_bias = torch.empty((T,), dtype=torch.float32, device=device)
+    _same_device(device, natoms=natoms, grad_weight=grad_weight, grad_bias=grad_bias)
+    ws, size = _scratch("mg_mx8_weight_gradient_workspace", device, B, N, T, E)
+    _launch("mg_mx8_weight_gradient", device, MX_FORMATS[packed.format], number, B, N, T, E, grad.data_ptr(), stride,
+            codes, scales, _ptr(natoms, torch.int32, "natoms", (B,)),
+            _ptr(grad_weight, torch.float32, "grad_weight", (T, E)),
+            _ptr(grad_bias, torch.float32, "grad_bias", (T,)), None if ws is None else ws.data_ptr(), size)
+    return grad_weight, grad_bias
+
+
+def _product_out(out, shape, dtype, device):
+    if out is None:
+        out = torch.empty(shape, dtype=dtype, device=device)
+    elif tuple(out.shape) != shape:
+        raise ValueError("out must have shape %s, got %s" % (shape, tuple(out.shape)))
+    elif out.dtype != dtype:
+        raise TypeError("out must be %s, got %s" % (dtype, out.dtype))
+    _same_device(device, out=out)
+    return out, _row_stride(out, "out")
+
+
+def mg_mx4_product(a: MXTensor, b: MXTensor, bias=None, dtype=torch.float32, out=None):
+    """``a`` [...,K] times ``b`` [N,K] transposed, plus ``bias`` [N] (float32): [...,N] of ``dtype``."""
+    device = a.codes.device
+    M, K, ac, asc = _mx_pointers(a, "a", ("e2m1",), device)
+    N, Kb, bc, bsc = _mx_pointers(b, "b", ("e2m1",), device)
+    if K != Kb:
+        raise ValueError("rows of a have %d numbers, rows of b %d" % (K, Kb))
+    dtype = out.dtype if out is not None else dtype
+    number = _number(dtype, "dtype")
+    out, stride = _product_out(out, a.shape[:-1] + (N,), dtype, device)
+    _same_device(device, bias=bias)
+    _launch("mg_mx4_product", device, number, M, N, K, ac, asc, bc, bsc, _ptr(bias, torch.float32, "bias", (N,)),
+            out.data_ptr(), stride)
+    return out
+
+
+def mg_mx4_linear(x, weight: MXTensor, bias=None, out=None):
+    """``x`` [...,K] (plain numbers, taken to "e2m1" by the call) times ``weight`` [N,K] transposed,
+    plus ``bias`` [N] (float32): [...,N] in the type of ``x``."""
+    device = x.device
+    N, K, wc, wsc = _mx_pointers(weight, "weight", ("e2m1",), device)
+    if x.shape[-1] != K:
+        raise ValueError("rows of x have %d numbers, rows of weight %d" % (x.shape[-1], K))
+    number, stride = _number(x.dtype, "x"), _row_stride(x, "x")
+    M = 1
+    for d in x.shape[:-1]:
+        M *= d
+    out, ostride = _product_out(out, tuple(x.shape[:-1]) + (N,), x.dtype, device)
+    _same_device(device, bias=bias)
+    ws, size = _scratch("mg_mx4_linear_workspace", device, M, N, K)
+    _launch("mg_mx4_linear", device, number, M, N, K, x.data_ptr(), stride, wc, wsc,
+            _ptr(bias, torch.float32, "bias", (N,)), out.data_ptr(), ostride,
+            None if ws is None else ws.data_ptr(), size)
+    return out
