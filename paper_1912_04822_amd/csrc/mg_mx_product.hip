@@ -6,6 +6,8 @@
 // Products of elements and scales are exact; sums are in float.
 //
 // The operands are given as (B, A), so a lane's four results are 4 neighbouring n of one row m of C.
+#include <type_traits>
+
 #include "mg_common.h"
 #include "mg_mx.h"
 #include "mg_mx_ops.h"
@@ -205,11 +207,194 @@ hipError_t direct(const ProductArgs &p, hipStream_t stream)
     return hipGetLastError();
 }
 
+// Large products: a workgroup of 4 wavefronts makes a 256 x 256 tile of C, each wavefront 128 x 128 of it
+// (8 x 8 tiles of 16 x 16 in 256 accumulator registers, one wavefront per SIMD).  Codes go through LDS, where
+// every byte is read by two wavefronts: per 128 k a wavefront issues 64 products (1024 cycles of its matrix
+// core) for 16 operands of 1 KB.
+//   - Two buffers of 128 k.  While a step's products run, the next step's operands are read from LDS and the
+//     codes of the step after that are on their way from memory to registers; they are written to LDS at the
+//     end of the step, before its one barrier.
+//   - A row's 64 bytes of a step lie in LDS as four pieces of 16, piece c at place c ^ (row / 4) % 4: the 16
+//     rows that a quarter of a wavefront reads at once then cover all banks.
+//   - Scales are taken for four steps at a time (16 bytes of a row); three byte permutes turn them into one
+//     register that holds a lane's scale of each of the four steps, which the instruction picks by its
+//     operand selector.
+// Codes past the end of k are zeros with scale 0 (a power of two), rows past M or N repeat the last one and
+// are not stored.
+constexpr int kTile = 256;
+
+__device__ inline uint32_t tile_place(uint32_t row, uint32_t piece) { return row * 4 + (piece ^ ((row >> 2) & 3)); }
+
+template <int Step> __device__ inline v4f product_step(v4u b, v4u a, v4f c, int sb, int sa)
+{
+    const v8i x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
+    const v8i y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kE2m1, kE2m1, Step, sb, Step, sa);
+}
+
+// Byte g of each of four words.
+__device__ inline int scale_bytes(v4u w, uint32_t pick)
+{
+    const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], pick), hi = __builtin_amdgcn_perm(w[3], w[2], pick);
+    return (int)__builtin_amdgcn_perm(hi, lo, 0x05040100u);
+}
+
+struct TileStage {
+    v4u a[4], b[4];
+};
+
+template <Num T>
+__global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int mtiles, int ntiles)
+{
+    __shared__ v4u lds_a[2][kTile * 4], lds_b[2][kTile * 4], lds_sa[kTile], lds_sb[kTile];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int r = lane & 15, g = lane >> 4;
+    const int wm = wave >> 1, wn = wave & 1;
+
+    // tiles in runs of 8 along m, and every XCD (workgroup number modulo 8) on a run of its own
+    const int total = mtiles * ntiles;
+    int id = blockIdx.x;
+    {
+        const int per = total / 8, extra = total % 8, xcd = id % 8;
+        id = xcd * per + min(xcd, extra) + id / 8;
+    }
+    const int band = id / (8 * ntiles), rows = min(8, mtiles - band * 8);
+    const int in = id - band * 8 * ntiles;
+    const int m0 = (band * 8 + in % rows) * kTile, n0 = (in / rows) * kTile;
+
+    const int steps = (p.blocks + 3) / 4;
+    const uint8_t *codes_a = (const uint8_t *)p.a;
+    uint32_t row_a[4], row_b[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = (tid >> 2) + 64 * i;
+        row_a[i] = (uint32_t)min(m0 + row, p.M - 1);
+        row_b[i] = (uint32_t)min(n0 + row, p.N - 1);
+    }
+    const int piece = tid & 3;
+
+    auto fetch = [&](int step, TileStage &s) {
+        const int blk = step * 4 + piece;
+        const bool in_row = blk < p.blocks;
+        const int64_t at = in_row ? 16 * blk : 0;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            s.a[i] = *(const v4u *)(codes_a + (int64_t)row_a[i] * p.pitch + at);
+            s.b[i] = *(const v4u *)(p.b + (int64_t)row_b[i] * p.pitch + at);
+        }
+        if (!in_row) {
+#pragma unroll
+            for (int i = 0; i < 4; ++i) s.a[i] = s.b[i] = v4u{0, 0, 0, 0};
+        }
+    };
+    auto put = [&](int buffer, const TileStage &s) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const uint32_t at = tile_place((tid >> 2) + 64 * i, piece);
+            lds_a[buffer][at] = s.a[i];
+            lds_b[buffer][at] = s.b[i];
+        }
+    };
+    auto fetch_scales = [&](int step, v4u &sa, v4u &sb) {       // of steps step .. step + 3
+        const uint8_t *a = p.a_scales + (int64_t)min(m0 + tid, p.M - 1) * p.scale_pitch + step * 4;
+        const uint8_t *b = p.b_scales + (int64_t)min(n0 + tid, p.N - 1) * p.scale_pitch + step * 4;
+        if (step * 4 + 16 <= p.blocks) {
+            __builtin_memcpy(&sa, a, 16);
+            __builtin_memcpy(&sb, b, 16);
+        } else {
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int left = p.blocks - (step + w) * 4;     // blocks of this word
+                const uint32_t mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                sa[w] = left > 0 ? *(const uint32_t *)(a + 4 * w) & mask : 0u;
+                sb[w] = left > 0 ? *(const uint32_t *)(b + 4 * w) & mask : 0u;
+            }
+        }
+    };
+
+    const uint32_t lane_at = tile_place(r, g);
+    struct Operands {
+        v4u a[8], b[8];
+    };
+    auto read = [&](int buffer, Operands &o) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            o.a[i] = lds_a[buffer][(wm * 8 + i) * 64 + lane_at];
+            o.b[i] = lds_b[buffer][(wn * 8 + i) * 64 + lane_at];
+        }
+    };
+
+    v4f acc[8][8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+
+    const uint32_t pick = (uint32_t)g | (uint32_t)(4 + g) << 8 | 0x0c0c0000u;
+    int sa[8], sb[8];
+    TileStage stage;
+    Operands now;
+    v4u fa, fb;
+    fetch(0, stage);
+    fetch_scales(0, fa, fb);
+    put(0, stage);
+    lds_sa[tid] = fa;
+    lds_sb[tid] = fb;
+    fetch(min(1, steps - 1), stage);
+    __syncthreads();
+    read(0, now);
+    for (int step0 = 0; step0 < steps; step0 += 4) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            sa[i] = scale_bytes(lds_sa[wm * 128 + 16 * i + r], pick);
+            sb[i] = scale_bytes(lds_sb[wn * 128 + 16 * i + r], pick);
+        }
+        fetch_scales(min(step0 + 4, steps - 1), fa, fb);
+        auto one = [&](auto which) {
+            constexpr int W = decltype(which)::value;
+            const int step = step0 + W;
+            if (step >= steps) return;
+            put((W + 1) & 1, stage);                    // step + 1, whose buffer was read two steps ago
+            fetch(min(step + 2, steps - 1), stage);
+#pragma unroll
+            for (int i = 0; i < 8; ++i)
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    acc[i][j] = product_step<W>(now.b[j], now.a[i], acc[i][j], sb[j], sa[i]);
+            if (W == 3) {
+                lds_sa[tid] = fa;
+                lds_sb[tid] = fb;
+            }
+            __syncthreads();
+            read((W + 1) & 1, now);
+        };
+        one(std::integral_constant<int, 0>{});
+        one(std::integral_constant<int, 1>{});
+        one(std::integral_constant<int, 2>{});
+        one(std::integral_constant<int, 3>{});
+    }
+
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            store_results<T>(p, m0 + wm * 128 + 16 * i + r, n0 + wn * 128 + 16 * j + 4 * g, acc[i][j]);
+}
+
+template <Num T>
+hipError_t tiled(const ProductArgs &p, hipStream_t stream)
+{
+    const int mtiles = (p.M + kTile - 1) / kTile, ntiles = (p.N + kTile - 1) / kTile;
+    hipLaunchKernelGGL((product_tile_kernel<T>), dim3(mtiles * ntiles), dim3(256), 0, stream, p, mtiles, ntiles);
+    return hipGetLastError();
+}
+
 template <Num T>
 hipError_t product_typed(const ProductArgs &p, hipStream_t stream)
 {
     if (p.M <= 64) return direct<T, false, 1, 1, 4, 4>(p, stream);
     if (p.N <= 32) return direct<T, false, 2, 2, 4, 1>(p, stream);
+    if ((int64_t)((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile) >= 64) return tiled<T>(p, stream);
     return direct<T, false, 4, 4, 4, 1>(p, stream);
 }
 
