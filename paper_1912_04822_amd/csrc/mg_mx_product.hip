@@ -19,6 +19,7 @@ namespace {
 using v4u = __attribute__((ext_vector_type(4))) uint32_t;
 using v8i = __attribute__((ext_vector_type(8))) int;
 using v4f = __attribute__((ext_vector_type(4))) float;
+using v16f = __attribute__((ext_vector_type(16))) float;
 
 constexpr int kE2m1 = 4;                // the instruction's code for the element type
 
@@ -118,6 +119,17 @@ __device__ inline Operand quantise_block(const ProductArgs &p, uint32_t row, int
     return o;
 }
 
+__device__ inline v4f load_bias(const ProductArgs &p, int n)
+{
+    v4f b = {0.0f, 0.0f, 0.0f, 0.0f};
+    if (p.bias) {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+            if (n + i < p.N) b[i] = p.bias[n + i];
+    }
+    return b;
+}
+
 // Four neighbouring results of row m.
 template <Num T>
 __device__ inline void store_results(const ProductArgs &p, int m, int n, v4f v)
@@ -125,12 +137,7 @@ __device__ inline void store_results(const ProductArgs &p, int m, int n, v4f v)
     using E = typename NumTraits<T>::type;
     if (m >= p.M || n >= p.N) return;
     E *to = (E *)p.c + (int64_t)m * p.c_stride + n;
-    E e[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const float b = p.bias && n + i < p.N ? p.bias[n + i] : 0.0f;
-        e[i] = (E)(v[i] + b);
-    }
+    const E e[4] = {(E)v[0], (E)v[1], (E)v[2], (E)v[3]};
     if (n + 4 <= p.N) {
         __builtin_memcpy(to, e, sizeof e);
     } else {
@@ -193,9 +200,11 @@ __global__ __launch_bounds__(64 * Waves) void product_kernel(ProductArgs p)
                 for (int w = 1; w < KW; ++w) acc[i][j] += sums[wave + w][i * RN + j][lane];
     }
 #pragma unroll
-    for (int i = 0; i < RM; ++i)
+    for (int j = 0; j < RN; ++j) {
+        const v4f bias = load_bias(p, n0 + 16 * j + 4 * g);
 #pragma unroll
-        for (int j = 0; j < RN; ++j) store_results<T>(p, m0 + 16 * i + r, n0 + 16 * j + 4 * g, acc[i][j]);
+        for (int i = 0; i < RM; ++i) store_results<T>(p, m0 + 16 * i + r, n0 + 16 * j + 4 * g, acc[i][j] + bias);
+    }
 }
 
 template <Num T, bool Plain, int RM, int RN, int Waves, int KW>
@@ -208,47 +217,69 @@ hipError_t direct(const ProductArgs &p, hipStream_t stream)
 }
 
 // Large products: a workgroup of 4 wavefronts makes a 256 x 256 tile of C, each wavefront 128 x 128 of it
-// (8 x 8 tiles of 16 x 16 in 256 accumulator registers, one wavefront per SIMD).  Codes go through LDS, where
-// every byte is read by two wavefronts: per 128 k a wavefront issues 64 products (1024 cycles of its matrix
-// core) for 16 operands of 1 KB.
-//   - Two buffers of 128 k.  While a step's products run, the next step's operands are read from LDS and the
-//     codes of the step after that are on their way from memory to registers; they are written to LDS at the
-//     end of the step, before its one barrier.
+// (4 x 4 tiles of 32 x 32 in 256 accumulator registers, one wavefront per SIMD) with
+// v_mfma_scale_f32_32x32x64_f8f6f4: from registers alone it reaches 9.0 PFLOP/s (6.3 with random codes, where
+// the chip lowers its clock), the 16 x 16 x 128 form 5.6 (4.9).  Codes go through LDS, where every byte is
+// read by two wavefronts: per 128 k a wavefront issues 32 products (1024 cycles of its matrix core) for 16
+// operands of 1 KB.
+//   - Four buffers of 128 k.  Codes go from memory to LDS without passing registers, four steps ahead, and
+//     from LDS to registers one step ahead, while the products of the step before run: neither is waited for
+//     in steady state.  A wavefront waits for its own loads of the next step only, then for the others at the
+//     step's one barrier.
 //   - A row's 64 bytes of a step lie in LDS as four pieces of 16, piece c at place c ^ (row / 4) % 4: the 16
 //     rows that a quarter of a wavefront reads at once then cover all banks.
-//   - Scales are taken for four steps at a time (16 bytes of a row); three byte permutes turn them into one
-//     register that holds a lane's scale of each of the four steps, which the instruction picks by its
-//     operand selector.
-// Codes past the end of k are zeros with scale 0 (a power of two), rows past M or N repeat the last one and
-// are not stored.
+//   - Scales are taken for four steps at a time (16 bytes of a row), a round of four steps ahead; three byte
+//     permutes turn them into one register that holds a lane's scale of each of the four steps, which the
+//     instruction picks by its operand selector.
+// Past the end of k the codes of A are zeros and the scales powers of two; rows past M or N repeat the last
+// one and are not stored.
 constexpr int kTile = 256;
 
 __device__ inline uint32_t tile_place(uint32_t row, uint32_t piece) { return row * 4 + (piece ^ ((row >> 2) & 3)); }
 
-template <int Step> __device__ inline v4f product_step(v4u b, v4u a, v4f c, int sb, int sa)
+template <int Step> __device__ inline v16f product_step(v4u b, v4u a, v16f c, int sb, int sa)
 {
     const v8i x = {(int)b[0], (int)b[1], (int)b[2], (int)b[3], 0, 0, 0, 0};
     const v8i y = {(int)a[0], (int)a[1], (int)a[2], (int)a[3], 0, 0, 0, 0};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(x, y, c, kE2m1, kE2m1, Step, sb, Step, sa);
+    return __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(x, y, c, kE2m1, kE2m1, Step, sb, Step, sa);
 }
 
-// Byte g of each of four words.
+// The byte that `pick` names of each of four words.
 __device__ inline int scale_bytes(v4u w, uint32_t pick)
 {
     const uint32_t lo = __builtin_amdgcn_perm(w[1], w[0], pick), hi = __builtin_amdgcn_perm(w[3], w[2], pick);
     return (int)__builtin_amdgcn_perm(hi, lo, 0x05040100u);
 }
 
-struct TileStage {
-    v4u a[4], b[4];
-};
+// 16 bytes per lane from memory (a common base, an offset per lane) to LDS, where they lie one lane after the
+// other.  Written as an instruction because the compiler would wait for every load under way before each read
+// of LDS; nothing is returned to registers, and wait_loads and the barrier stand before the first read of
+// what was loaded.  The address in LDS goes by m0, which is put back.
+__device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t lds)
+{
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "v"(offset), "s"(base), "s"(lds) : "memory");
+}
+__device__ inline uint32_t lds_address(const v4u *p)
+{
+    return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p);
+}
+
+// Waits until at most N of this wavefront's loads are under way, and for its LDS accesses.
+template <int N> __device__ inline void wait_loads()
+{
+    __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4) << 14);
+}
 
 template <Num T>
 __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int mtiles, int ntiles)
 {
-    __shared__ v4u lds_a[2][kTile * 4], lds_b[2][kTile * 4], lds_sa[kTile], lds_sb[kTile];
+    constexpr int kBuffer = kTile * 8;                      // 16-byte pieces of a buffer: codes of A, then of B
+    __shared__ v4u lds[4 * kBuffer + 2 * kTile];            // then 16 bytes of scales for every row of A and B
+    v4u *const lds_sa = lds + 4 * kBuffer, *const lds_sb = lds_sa + kTile;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int r = lane & 15, g = lane >> 4;
+    const int r = lane & 31, h = lane >> 5;                 // an operand: row r, the h-th 32 of its 64 k
     const int wm = wave >> 1, wn = wave & 1;
 
     // tiles in runs of 8 along m, and every XCD (workgroup number modulo 8) on a run of its own
@@ -263,110 +294,131 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
     const int m0 = (band * 8 + in % rows) * kTile, n0 = (in / rows) * kTile;
 
     const int steps = (p.blocks + 3) / 4;
-    const uint8_t *codes_a = (const uint8_t *)p.a;
-    uint32_t row_a[4], row_b[4];
+    const uint8_t *const base_a = (const uint8_t *)p.a + (int64_t)m0 * p.pitch;
+    const uint8_t *const base_b = p.b + (int64_t)n0 * p.pitch;
+    const uint32_t piece = (lane & 3) ^ (lane >> 4);        // see tile_place: row / 4 = lane / 16 modulo 4
+    uint32_t off_a[4], off_b[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-        const int row = (tid >> 2) + 64 * i;
-        row_a[i] = (uint32_t)min(m0 + row, p.M - 1);
-        row_b[i] = (uint32_t)min(n0 + row, p.N - 1);
+        const int row = (4 * i + wave) * 16 + (lane >> 2);
+        off_a[i] = (uint32_t)min(row, p.M - 1 - m0) * p.pitch + 16 * piece;
+        off_b[i] = (uint32_t)min(row, p.N - 1 - n0) * p.pitch + 16 * piece;
     }
-    const int piece = tid & 3;
-
-    auto fetch = [&](int step, TileStage &s) {
-        const int blk = step * 4 + piece;
-        const bool in_row = blk < p.blocks;
-        const int64_t at = in_row ? 16 * blk : 0;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            s.a[i] = *(const v4u *)(codes_a + (int64_t)row_a[i] * p.pitch + at);
-            s.b[i] = *(const v4u *)(p.b + (int64_t)row_b[i] * p.pitch + at);
-        }
-        if (!in_row) {
-#pragma unroll
-            for (int i = 0; i < 4; ++i) s.a[i] = s.b[i] = v4u{0, 0, 0, 0};
-        }
+    const uint32_t put = lds_address(lds) + wave * 1024;
+    // one of the eight loads of a step: 16 rows of A (0 .. 3) or B per wavefront
+    auto fetch = [&](int step, int buffer, int which, uint32_t back) {
+        const uint32_t to = put + (buffer * kBuffer + which * kTile) * 16;
+        if (which < 4) load_to_lds(base_a + step * 64, off_a[which] - back, to);
+        else load_to_lds(base_b + step * 64, off_b[which - 4] - back, to);
     };
-    auto put = [&](int buffer, const TileStage &s) {
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-            const uint32_t at = tile_place((tid >> 2) + 64 * i, piece);
-            lds_a[buffer][at] = s.a[i];
-            lds_b[buffer][at] = s.b[i];
-        }
-    };
-    auto fetch_scales = [&](int step, v4u &sa, v4u &sb) {       // of steps step .. step + 3
-        const uint8_t *a = p.a_scales + (int64_t)min(m0 + tid, p.M - 1) * p.scale_pitch + step * 4;
-        const uint8_t *b = p.b_scales + (int64_t)min(n0 + tid, p.N - 1) * p.scale_pitch + step * 4;
+    // pieces past a row's end are not read: the lane takes the step's first piece, which its row has
+    auto past_end = [&](int step) { return step * 4 + (int)piece < p.blocks ? 0u : 16 * piece; };
+    const uint32_t scale_off_a = (uint32_t)min(tid, p.M - 1 - m0) * p.scale_pitch;
+    const uint32_t scale_off_b = (uint32_t)min(tid, p.N - 1 - n0) * p.scale_pitch;
+    const uint8_t *const scale_a = p.a_scales + (int64_t)m0 * p.scale_pitch;
+    const uint8_t *const scale_b = p.b_scales + (int64_t)n0 * p.scale_pitch;
+    const uint32_t put_sa = lds_address(lds_sa) + wave * 1024, put_sb = lds_address(lds_sb) + wave * 1024;
+    auto fetch_scales = [&](int step) {                     // of steps step .. step + 3
         if (step * 4 + 16 <= p.blocks) {
-            __builtin_memcpy(&sa, a, 16);
-            __builtin_memcpy(&sb, b, 16);
-        } else {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) {
-                const int left = p.blocks - (step + w) * 4;     // blocks of this word
-                const uint32_t mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-                sa[w] = left > 0 ? *(const uint32_t *)(a + 4 * w) & mask : 0u;
-                sb[w] = left > 0 ? *(const uint32_t *)(b + 4 * w) & mask : 0u;
-            }
+            load_to_lds(scale_a + step * 4, scale_off_a, put_sa);
+            load_to_lds(scale_b + step * 4, scale_off_b, put_sb);
+            return;
         }
+        v4u sa, sb;                                         // a row's end: bytes past it become zeros
+#pragma unroll
+        for (int w = 0; w < 4; ++w) {
+            const int left = p.blocks - (step + w) * 4;     // blocks of this word
+            const uint32_t mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+            sa[w] = left > 0 ? *(const uint32_t *)(scale_a + scale_off_a + (step + w) * 4) & mask : 0u;
+            sb[w] = left > 0 ? *(const uint32_t *)(scale_b + scale_off_b + (step + w) * 4) & mask : 0u;
+        }
+        lds_sa[tid] = sa;
+        lds_sb[tid] = sb;
     };
 
-    const uint32_t lane_at = tile_place(r, g);
+    const uint32_t lane_at[2] = {tile_place(r, h), tile_place(r, 2 + h)};       // first and second 64 k
     struct Operands {
-        v4u a[8], b[8];
+        v4u a[2][4], b[2][4];
     };
-    auto read = [&](int buffer, Operands &o) {
+    auto read = [&](int buffer, int which, Operands &o) {   // one of sixteen
+        const v4u *from = lds + buffer * kBuffer;
+        const int k = which >> 3, i = which & 3;
+        if (which & 4) o.a[k][i] = from[(wm * 4 + i) * 128 + lane_at[k]];
+        else o.b[k][i] = from[kTile * 4 + (wn * 4 + i) * 128 + lane_at[k]];
+    };
+    const uint32_t pick = (uint32_t)h | (uint32_t)(4 + h) << 8 | 0x0c0c0000u;
+    struct Scales {
+        int a[2][4], b[2][4];
+    };
+    auto read_scales = [&](int i, Scales &s) {              // one of the four rows of tiles
+        const v4u a = lds_sa[wm * 128 + 32 * i + r], b = lds_sb[wn * 128 + 32 * i + r];
+        s.a[0][i] = scale_bytes(a, pick);
+        s.b[0][i] = scale_bytes(b, pick);
+        s.a[1][i] = scale_bytes(a, pick + 0x0202u);
+        s.b[1][i] = scale_bytes(b, pick + 0x0202u);
+    };
+
+    v16f acc[4][4];
 #pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            o.a[i] = lds_a[buffer][(wm * 8 + i) * 64 + lane_at];
-            o.b[i] = lds_b[buffer][(wn * 8 + i) * 64 + lane_at];
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
+
+    Scales scales, later;
+    Operands even, odd;
+    fetch_scales(0);
+#pragma unroll
+    for (int s = 0; s < 4; ++s)
+        if (s < steps) {
+            const uint32_t back = past_end(s);
+#pragma unroll
+            for (int q = 0; q < 8; ++q) fetch(s, s, q, back);
         }
-    };
-
-    v4f acc[8][8];
+    if (steps > 3) wait_loads<24>();
+    else wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int q = 0; q < 16; ++q) read(0, q, even);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) acc[i][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    for (int i = 0; i < 4; ++i) read_scales(i, later);
 
-    const uint32_t pick = (uint32_t)g | (uint32_t)(4 + g) << 8 | 0x0c0c0000u;
-    int sa[8], sb[8];
-    TileStage stage;
-    Operands now;
-    v4u fa, fb;
-    fetch(0, stage);
-    fetch_scales(0, fa, fb);
-    put(0, stage);
-    lds_sa[tid] = fa;
-    lds_sb[tid] = fb;
-    fetch(min(1, steps - 1), stage);
-    __syncthreads();
-    read(0, now);
     for (int step0 = 0; step0 < steps; step0 += 4) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            sa[i] = scale_bytes(lds_sa[wm * 128 + 16 * i + r], pick);
-            sb[i] = scale_bytes(lds_sb[wn * 128 + 16 * i + r], pick);
-        }
-        fetch_scales(min(step0 + 4, steps - 1), fa, fb);
+        scales = later;
+        // One step.  At its barrier this step's operands are in registers in every wavefront and the next
+        // step's codes in LDS; between the products the next step's operands are read and the codes four
+        // steps on are asked for (the last step's again where there are none: the count of loads under way
+        // stays the same, and nothing reads them).  The order is pinned: a wavefront issues one instruction
+        // at a time, and everything else has to fit between two products.
         auto one = [&](auto which) {
             constexpr int W = decltype(which)::value;
             const int step = step0 + W;
             if (step >= steps) return;
-            put((W + 1) & 1, stage);                    // step + 1, whose buffer was read two steps ago
-            fetch(min(step + 2, steps - 1), stage);
+            Operands &now = W & 1 ? odd : even, &next = W & 1 ? even : odd;
+            wait_loads<16>();
+            __builtin_amdgcn_s_barrier();
+            if (W == 0 && step + 4 < steps) fetch_scales(step + 4);
+            const int ahead = min(step + 4, steps - 1);
+            const uint32_t back = past_end(ahead);
+            if (step * 4 + 4 > p.blocks) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i)
+                for (int k = 0; k < 2; ++k) {
+                    const bool in_row = step * 4 + 2 * k + h < p.blocks;
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    acc[i][j] = product_step<W>(now.b[j], now.a[i], acc[i][j], sb[j], sa[i]);
-            if (W == 3) {
-                lds_sa[tid] = fa;
-                lds_sb[tid] = fb;
+                    for (int i = 0; i < 4; ++i) now.a[k][i] = in_row ? now.a[k][i] : v4u{0, 0, 0, 0};
+                }
             }
-            __syncthreads();
-            read((W + 1) & 1, now);
+            __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+            for (int t = 0; t < 32; ++t) {
+                const int k = t >> 4, i = (t >> 2) & 3, j = t & 3;
+                acc[i][j] = product_step<W>(now.b[k][j], now.a[k][i], acc[i][j], scales.b[k][j], scales.a[k][i]);
+                if (t < 16) read((W + 1) & 3, t, next);
+                if (t >= 16 && (t & 1) == 0) fetch(ahead, W, (t - 16) >> 1, back);
+                if (W >= 2 && (t == 19 || t == 27)) read_scales((W - 2) * 2 + (t == 27), later);
+                __builtin_amdgcn_sched_barrier(0);
+            }
         };
         one(std::integral_constant<int, 0>{});
         one(std::integral_constant<int, 1>{});
@@ -374,11 +426,51 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
         one(std::integral_constant<int, 3>{});
     }
 
+    // A wavefront turns its results through LDS, 32 rows of 128 at a time (rows 16 bytes further apart, so
+    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch.
+    using E = typename NumTraits<T>::type;
+    constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 128 / P, kPitch = 132;
+    wait_loads<0>();
+    __builtin_amdgcn_s_barrier();
+    float *const mine = (float *)(lds + wave * kBuffer);
+    const int col = P * (lane % kLanes), n = n0 + wn * 128 + col;
+    float bias[P];
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
+    for (int e = 0; e < P; ++e) bias[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
 #pragma unroll
-        for (int j = 0; j < 8; ++j)
-            store_results<T>(p, m0 + wm * 128 + 16 * i + r, n0 + wn * 128 + 16 * j + 4 * g, acc[i][j]);
+    for (int i = 0; i < 4; ++i) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+                const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
+                *(v4f *)(mine + r * kPitch + 32 * j + 8 * q + 4 * h) = v;
+            }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+#pragma unroll
+        for (int t = 0; t < 32 * kLanes / 64; ++t) {
+            const int row = t * (64 / kLanes) + lane / kLanes;
+            const float *from = mine + row * kPitch + col;
+            E e[P];
+#pragma unroll
+            for (int c = 0; c < P; c += 4) {
+                const v4f v = *(const v4f *)(from + c);
+#pragma unroll
+                for (int d = 0; d < 4; ++d) e[c + d] = (E)(v[d] + bias[c + d]);
+            }
+            const int m = m0 + wm * 128 + 32 * i + row;
+            if (m >= p.M) continue;
+            E *to = (E *)p.c + (int64_t)m * p.c_stride + n;
+            if (n + P <= p.N) {
+                __builtin_memcpy(to, e, 16);
+            } else {
+#pragma unroll
+                for (int d = 0; d < P; ++d)
+                    if (n + d < p.N) to[d] = e[d];
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    }
 }
 
 template <Num T>
