@@ -588,7 +588,7 @@ int mg_mx8_weight_gradient(int format, int dtype, int B, int N, int T, int E, co
     if ((format != MG_MX_INT8 && format != MG_MX_E4M3) || !mx_type(dtype)) return MG_EPARAM;
     const int rc = check_mx_gradient(B, N, T, E);
     if (rc != MG_OK) return rc;
-    if (grad_stride < T || grad_stride > ((int64_t)1 << 40)) return MG_ESHAPE;
+    if (grad_stride < T || grad_stride > ((int64_t)1 << 26)) return MG_ESHAPE;
     if (misaligned_number(grad, dtype) || misaligned_codes(codes, scales) || misaligned4(natoms) ||
         misaligned4(grad_weight) || misaligned4(grad_bias))
         return MG_EALIGN;
