@@ -77,11 +77,11 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
     // columns and channels past the end read the last valid ones and are not stored
     const uint32_t col = min((uint32_t)(etile * kCols + 4 * Words * c), a.code_pitch - 4 * Words);
     const uint32_t block = col / kMxBlock, shift = 8 * (block & 3);
-    uint32_t code_at[8], scale_at[8], grad_at[8], chan[CT];
+    uint32_t code_at[8], grad_at[8], chan[CT];
+    const uint32_t scale_at = 8 * h * a.scale_pitch + (block & ~3u);
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
         code_at[i] = (8 * h + i) * a.code_pitch + col;
-        scale_at[i] = (8 * h + i) * a.scale_pitch + (block & ~3u);
         grad_at[i] = (8 * h + i) * a.grad_stride;
     }
 #pragma unroll
@@ -114,13 +114,13 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
         };
         if (a.M - m0 >= kRows) {
 #pragma unroll
-            for (int i = 0; i < 8; ++i) get(i, code_at[i], scale_at[i], grad_at[i]);
+            for (int i = 0; i < 8; ++i) get(i, code_at[i], scale_at + i * a.scale_pitch, grad_at[i]);
         } else {                            // the last step: rows past the end read the last row
             const uint32_t last = a.M - 1 - m0;
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const uint32_t over = max((uint32_t)(8 * h + i), last) - last;
-                get(i, code_at[i] - over * a.code_pitch, scale_at[i] - over * a.scale_pitch,
+                get(i, code_at[i] - over * a.code_pitch, scale_at + i * a.scale_pitch - over * a.scale_pitch,
                     grad_at[i] - over * a.grad_stride);
             }
         }

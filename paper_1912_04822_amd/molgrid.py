@@ -482,34 +482,61 @@ class MXTensor:
 
 def _mx_layout(shape, format):
     """(rows, columns), shapes of codes and scales."""
-    if format not in MX_FORMATS:
+    per_block = _BLOCK_BYTES.get(format)
+    if per_block is None:
         raise ValueError("format must be one of %s, got %r" % (", ".join(MX_FORMATS), format))
-    if len(shape) == 0:
+    if len(shape) == 2:
+        rows, cols = shape
+    elif len(shape) == 0:
         raise ValueError("a tensor in a microscaled format has at least one dimension")
-    rows, cols = 1, shape[-1]
-    for d in shape[:-1]:
-        rows *= d
-    blocks = (cols + 31) // 32
-    return rows, cols, (rows, blocks * (16 if format == "e2m1" else 32)), (rows, (blocks + 3) // 4 * 4)
+    else:
+        rows, cols = 1, shape[-1]
+        for d in shape[:-1]:
+            rows *= d
+    blocks = (cols + 31) >> 5
+    return rows, cols, (rows, blocks * per_block), (rows, (blocks + 3) & ~3)
 
 
-def _mx_pointers(t, name, formats, device):
+_BLOCK_BYTES = {"int8": 32, "e4m3": 32, "e2m1": 16}
+
+
+def _mx_pointers(t, name, formats, dev):
     """Checks an MXTensor; (rows, columns, codes, scales)."""
     if not isinstance(t, MXTensor):
         raise TypeError("%s must be an MXTensor, got %s" % (name, type(t).__name__))
     if t.format not in formats:
         raise ValueError("%s must be in %s, got %s" % (name, " or ".join(formats), t.format))
     rows, cols, cshape, sshape = _mx_layout(t.shape, t.format)
-    codes = _ptr(t.codes, torch.uint8, name + ".codes", cshape)
-    scales = _ptr(t.scales, torch.uint8, name + ".scales", sshape)
-    _same_device(device, **{name + ".codes": t.codes, name + ".scales": t.scales})
-    return rows, cols, codes, scales
+    codes, scales = t.codes, t.scales
+    if codes.get_device() != dev or scales.get_device() != dev:
+        _refuse_device(dev, **{name + ".codes": codes, name + ".scales": scales})
+    return (rows, cols, _ptr(codes, torch.uint8, name + ".codes", cshape),
+            _ptr(scales, torch.uint8, name + ".scales", sshape))
 
 
-def _same_device(device, **tensors):
+def _device(t, name):
+    """Number of the device a tensor is on."""
+    dev = t.get_device()
+    if dev < 0 or not t.is_cuda:
+        raise ValueError("%s must be a device tensor" % name)
+    return dev
+
+
+def _refuse_device(dev, **tensors):
     for name, t in tensors.items():
-        if t is not None and t.device != device:
-            raise ValueError("%s is on %s, not on %s" % (name, t.device, device))
+        if t.get_device() != dev:
+            if not t.is_cuda:
+                raise ValueError("%s must be a device tensor" % name)
+            raise ValueError("%s is on device %d, not on %d" % (name, t.get_device(), dev))
+
+
+def _optional(t, dtype, name, shape, dev):
+    """Address of an array that may be missing, on the call's device."""
+    if t is None:
+        return None
+    if t.get_device() != dev:
+        _refuse_device(dev, **{name: t})
+    return _ptr(t, dtype, name, shape)
 
 
 def _number(dtype, name):
@@ -521,13 +548,11 @@ def _number(dtype, name):
 
 def _row_stride(t, name):
     """Elements from row to row of a tensor whose rows (last dimension) are equally far apart."""
-    if not t.is_cuda:
-        raise ValueError("%s must be a device tensor" % name)
     if t.is_contiguous():
         return t.shape[-1]
     if t.shape[-1] > 1 and t.stride(-1) != 1:
         raise ValueError("the last dimension of %s must be contiguous" % name)
-    step = None
+    step = unit = None
     for d in range(t.dim() - 2, -1, -1):        # the innermost dimension that has a step fixes it
         if t.shape[d] == 1:
             continue
@@ -543,65 +568,62 @@ def _row_stride(t, name):
     return step
 
 
-def _on(device):
-    """Launches go to the tensors' device, whichever is current."""
-    return torch.cuda.device(device)
+# torch's own short way to the number of the current device
+_current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
 
-def _current(device):
-    return device.index == torch.cuda.current_device()
-
-
-def _launch(name, device, *args):
-    """One library call on the device's current stream."""
-    fn = getattr(lib(), name)
-    if _current(device):
-        rc = fn(*args, _stream())
+def _launch(fn, dev, *args):
+    """One library call on the current stream of the tensors' device, whichever device is current."""
+    if dev == _current_device():
+        rc = fn(*args, _raw_stream(dev) if _raw_stream is not None else _stream())
     else:
-        with _on(device):
+        with torch.cuda.device(dev):
             rc = fn(*args, _stream())
     if rc != MG_OK:
-        raise MolgridError(rc, name)
+        raise MolgridError(rc, fn.__name__)
 
 
-def _scratch(name, device, *sizes):
-    """The workspace a call of these sizes needs (bytes from ``name``), or None."""
+def _workspace_of(fn, like, *sizes):
+    """The workspace a call of these sizes needs (bytes from ``fn``), and its size.  A new one for
+    every call: calls on several streams, or captured in several graphs, share none."""
     n = ctypes.c_size_t()
-    rc = getattr(lib(), name)(*sizes, ctypes.byref(n))
+    rc = fn(*sizes, ctypes.byref(n))
     if rc != MG_OK:
-        raise MolgridError(rc, name)
-    return (torch.empty(n.value, dtype=torch.uint8, device=device) if n.value else None), n.value
+        raise MolgridError(rc, fn.__name__)
+    return (like.new_empty(n.value, dtype=torch.uint8) if n.value else None), n.value
 
 
 def mg_mx_pack(x, format="int8", out: Optional[MXTensor] = None) -> MXTensor:
     """``x`` (float32, float16 or bfloat16; rows along the last dimension, equally far apart) in
     blocks of 32 numbers that share a power of two."""
-    rows, cols, cshape, sshape = _mx_layout(x.shape, format)
-    dtype, stride = _number(x.dtype, "x"), _row_stride(x, "x")
+    shape = x.shape
+    rows, cols, cshape, sshape = _mx_layout(shape, format)
+    dtype, stride, dev = _number(x.dtype, "x"), _row_stride(x, "x"), _device(x, "x")
     if out is None:
-        out = MXTensor(torch.empty(cshape, dtype=torch.uint8, device=x.device),
-                       torch.empty(sshape, dtype=torch.uint8, device=x.device), x.shape, format, x.dtype)
+        out = MXTensor(x.new_empty(cshape, dtype=torch.uint8), x.new_empty(sshape, dtype=torch.uint8), shape,
+                       format, x.dtype)
         codes, scales = out.codes.data_ptr(), out.scales.data_ptr()
     else:
-        if out.shape != tuple(x.shape):
-            raise ValueError("out must have shape %s, got %s" % (tuple(x.shape), out.shape))
-        _, _, codes, scales = _mx_pointers(out, "out", (format,), x.device)
+        if out.shape != tuple(shape):
+            raise ValueError("out must have shape %s, got %s" % (tuple(shape), out.shape))
+        _, _, codes, scales = _mx_pointers(out, "out", (format,), dev)
         out.dtype = x.dtype
-    _launch("mg_mx_pack", x.device, MX_FORMATS[format], dtype, rows, cols, x.data_ptr(), stride, codes, scales)
+    _launch(lib().mg_mx_pack, dev, MX_FORMATS[format], dtype, rows, cols, x.data_ptr(), stride, codes, scales)
     return out
 
 
 def mg_mx_unpack(packed: MXTensor, dtype=None, out=None):
     """The numbers ``packed`` stands for, as a tensor of its shape (``dtype``: default its own)."""
-    device = packed.codes.device
-    rows, cols, codes, scales = _mx_pointers(packed, "packed", tuple(MX_FORMATS), device)
+    dev = _device(packed.codes, "packed.codes")
+    rows, cols, codes, scales = _mx_pointers(packed, "packed", MX_FORMATS, dev)
     if out is None:
-        out = torch.empty(packed.shape, dtype=dtype or packed.dtype, device=device)
+        out = packed.codes.new_empty(packed.shape, dtype=dtype or packed.dtype)
     elif tuple(out.shape) != packed.shape:
         raise ValueError("out must have shape %s, got %s" % (packed.shape, tuple(out.shape)))
     number, stride = _number(out.dtype, "out"), _row_stride(out, "out")
-    _same_device(device, out=out)
-    _launch("mg_mx_unpack", device, MX_FORMATS[packed.format], number, rows, cols, codes, scales, out.data_ptr(),
+    if out.get_device() != dev:
+        _refuse_device(dev, out=out)
+    _launch(lib().mg_mx_unpack, dev, MX_FORMATS[packed.format], number, rows, cols, codes, scales, out.data_ptr(),
             stride)
     return out
 
@@ -610,8 +632,8 @@ def mg_mx8_weight_gradient(grad, packed: MXTensor, natoms=None, grad_weight=None
     """(``grad_weight`` [T,E], ``grad_bias`` [T]) in float32 of y = x W^T + b, from ``grad`` [...,T]
     on y and the 8-bit codes of x [...,E].  ``natoms`` [B] (x of shape [B,N,E]): atoms past it
     count for nothing, whatever their rows hold."""
-    device = grad.device
-    rows, E, codes, scales = _mx_pointers(packed, "packed", ("int8", "e4m3"), device)
+    dev = grad.get_device()
+    rows, E, codes, scales = _mx_pointers(packed, "packed", ("int8", "e4m3"), dev)
     T = grad.shape[-1]
     if tuple(grad.shape[:-1]) != packed.shape[:-1]:
         raise ValueError("grad must have shape %s, got %s" % (packed.shape[:-1] + (T,), tuple(grad.shape)))
@@ -619,61 +641,63 @@ def mg_mx8_weight_gradient(grad, packed: MXTensor, natoms=None, grad_weight=None
     if natoms is not None and len(packed.shape) != 3:
         raise ValueError("natoms needs x of shape [B,N,E], got %s" % (packed.shape,))
     number, stride = _number(grad.dtype, "grad"), _row_stride(grad, "grad")
+    L = lib()
+    ws, size = _workspace_of(L.mg_mx8_weight_gradient_workspace, grad, B, N, T, E)
     if grad_weight is None:
-        grad_weight = torch.empty((T, E), dtype=torch.float32, device=device)
+        grad_weight = grad.new_empty((T, E), dtype=torch.float32)
     if grad_bias is None:
-        grad_bias = torch.empty((T,), dtype=torch.float32, device=device)
-    _same_device(device, natoms=natoms, grad_weight=grad_weight, grad_bias=grad_bias)
-    ws, size = _scratch("mg_mx8_weight_gradient_workspace", device, B, N, T, E)
-    _launch("mg_mx8_weight_gradient", device, MX_FORMATS[packed.format], number, B, N, T, E, grad.data_ptr(), stride,
-            codes, scales, _ptr(natoms, torch.int32, "natoms", (B,)),
-            _ptr(grad_weight, torch.float32, "grad_weight", (T, E)),
-            _ptr(grad_bias, torch.float32, "grad_bias", (T,)), None if ws is None else ws.data_ptr(), size)
+        grad_bias = grad.new_empty((T,), dtype=torch.float32)
+    _launch(L.mg_mx8_weight_gradient, dev, MX_FORMATS[packed.format], number, B, N, T, E, grad.data_ptr(), stride,
+            codes, scales, _optional(natoms, torch.int32, "natoms", (B,), dev),
+            _optional(grad_weight, torch.float32, "grad_weight", (T, E), dev),
+            _optional(grad_bias, torch.float32, "grad_bias", (T,), dev), None if ws is None else ws.data_ptr(), size)
     return grad_weight, grad_bias
 
 
-def _product_out(out, shape, dtype, device):
+def _product_out(out, shape, dtype, like, dev):
+    """The result's tensor and the stride of its rows."""
     if out is None:
-        out = torch.empty(shape, dtype=dtype, device=device)
-    elif tuple(out.shape) != shape:
+        return like.new_empty(shape, dtype=dtype), shape[-1]
+    if tuple(out.shape) != shape:
         raise ValueError("out must have shape %s, got %s" % (shape, tuple(out.shape)))
-    elif out.dtype != dtype:
+    if out.dtype != dtype:
         raise TypeError("out must be %s, got %s" % (dtype, out.dtype))
-    _same_device(device, out=out)
+    if out.get_device() != dev:
+        _refuse_device(dev, out=out)
     return out, _row_stride(out, "out")
 
 
 def mg_mx4_product(a: MXTensor, b: MXTensor, bias=None, dtype=torch.float32, out=None):
     """``a`` [...,K] times ``b`` [N,K] transposed, plus ``bias`` [N] (float32): [...,N] of ``dtype``."""
-    device = a.codes.device
-    M, K, ac, asc = _mx_pointers(a, "a", ("e2m1",), device)
-    N, Kb, bc, bsc = _mx_pointers(b, "b", ("e2m1",), device)
+    dev = _device(a.codes, "a.codes")
+    M, K, ac, asc = _mx_pointers(a, "a", ("e2m1",), dev)
+    N, Kb, bc, bsc = _mx_pointers(b, "b", ("e2m1",), dev)
     if K != Kb:
         raise ValueError("rows of a have %d numbers, rows of b %d" % (K, Kb))
     dtype = out.dtype if out is not None else dtype
     number = _number(dtype, "dtype")
-    out, stride = _product_out(out, a.shape[:-1] + (N,), dtype, device)
-    _same_device(device, bias=bias)
-    _launch("mg_mx4_product", device, number, M, N, K, ac, asc, bc, bsc, _ptr(bias, torch.float32, "bias", (N,)),
-            out.data_ptr(), stride)
+    out, stride = _product_out(out, a.shape[:-1] + (N,), dtype, a.codes, dev)
+    _launch(lib().mg_mx4_product, dev, number, M, N, K, ac, asc, bc, bsc,
+            _optional(bias, torch.float32, "bias", (N,), dev), out.data_ptr(), stride)
     return out
 
 
 def mg_mx4_linear(x, weight: MXTensor, bias=None, out=None):
     """``x`` [...,K] (plain numbers, taken to "e2m1" by the call) times ``weight`` [N,K] transposed,
     plus ``bias`` [N] (float32): [...,N] in the type of ``x``."""
-    device = x.device
-    N, K, wc, wsc = _mx_pointers(weight, "weight", ("e2m1",), device)
-    if x.shape[-1] != K:
-        raise ValueError("rows of x have %d numbers, rows of weight %d" % (x.shape[-1], K))
+    dev = x.get_device()
+    N, K, wc, wsc = _mx_pointers(weight, "weight", ("e2m1",), dev)
+    shape = x.shape
+    if shape[-1] != K:
+        raise ValueError("rows of x have %d numbers, rows of weight %d" % (shape[-1], K))
     number, stride = _number(x.dtype, "x"), _row_stride(x, "x")
     M = 1
-    for d in x.shape[:-1]:
+    for d in shape[:-1]:
         M *= d
-    out, ostride = _product_out(out, tuple(x.shape[:-1]) + (N,), x.dtype, device)
-    _same_device(device, bias=bias)
-    ws, size = _scratch("mg_mx4_linear_workspace", device, M, N, K)
-    _launch("mg_mx4_linear", device, number, M, N, K, x.data_ptr(), stride, wc, wsc,
-            _ptr(bias, torch.float32, "bias", (N,)), out.data_ptr(), ostride,
+    out, ostride = _product_out(out, tuple(shape[:-1]) + (N,), x.dtype, x, dev)
+    L = lib()
+    ws, size = _workspace_of(L.mg_mx4_linear_workspace, x, M, N, K)
+    _launch(L.mg_mx4_linear, dev, number, M, N, K, x.data_ptr(), stride, wc, wsc,
+            _optional(bias, torch.float32, "bias", (N,), dev), out.data_ptr(), ostride,
             None if ws is None else ws.data_ptr(), size)
     return out
