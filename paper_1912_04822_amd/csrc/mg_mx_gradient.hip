@@ -1,13 +1,15 @@
 // Weight gradient of a linear map from the 8-bit codes of its input (formats: mg_mx.h):
 //     dW[t][e] = sum over live rows m of G[m][t] X[m][e],     db[t] = sum over live rows of G[m][t].
 // X is M x E codes and by far the largest operand, T (channels) is small: what bounds the kernel is
-// reading the codes once.  A wavefront therefore keeps a 32 x 256 (32 x 128, 64 x 128) piece of dW in its
-// accumulators and walks down the rows, 16 at a time, with v_mfma_f32_32x32x16_bf16.
+// reading the codes once.  A wavefront therefore keeps a 32 x 256 piece of dW (16 to 64 channels) in its
+// accumulators and walks down the rows, 32 at a time, with v_mfma_f32_16x16x32_bf16.
 //   - The sum runs over rows, so the matrix operands want 8 consecutive ROWS of one column per lane
 //     while memory holds rows.  Which column of dW a matrix column stands for is free: lane c takes
-//     columns 4c..4c+3, one word of codes per row, and byte j of its 8 words (one per row) is its
-//     operand of the j-th of four products.  No transpose through LDS, no exchange between lanes, and
-//     the results of the four products are 4 neighbouring numbers of dW.
+//     columns 16c..16c+15, 16 bytes of codes per row, and byte j of its 8 rows is its operand of the j-th
+//     of sixteen products.  No transpose through LDS, and the results of the products are neighbouring
+//     numbers of dW.  Channels likewise: a lane loads 2 (4) neighbours of a row for 2 (4) operands.
+//   - A wavefront can have 63 loads under way: loads are as wide as can be (17 a step of 32 rows and 256
+//     columns), the scales come in one word per lane and go to the lanes that need them by an exchange.
 //   - A code times its power of two is exact in bfloat16 (at most 8 significant bits); blocks whose
 //     scale byte is 0 (magnitudes below 2^-120) count as zero.  A float gradient is cut into three
 //     bfloat16 pieces (8 + 8 + 8 bits, exact), a half one into two, so that the products are exact and
@@ -26,12 +28,12 @@ namespace mg {
 namespace {
 
 constexpr int kWaves = 8, kThreads = 64 * kWaves;
-constexpr int kRows = 16;               // rows of one step
-constexpr int kChanTile = 32;           // rows of dW per matrix product
+constexpr int kRows = 32;               // rows of one step
+constexpr int kDepth = 2;               // steps a wavefront holds: one it works on, the rest under way
 
 using v4u = __attribute__((ext_vector_type(4))) uint32_t;
 using v8bf = __attribute__((ext_vector_type(8))) __bf16;
-using v16f = __attribute__((ext_vector_type(16))) float;
+using v4f = __attribute__((ext_vector_type(4))) float;
 
 template <Num T> constexpr int kPieces = T == Num::F32 ? 3 : T == Num::F16 ? 2 : 1;
 
@@ -56,36 +58,51 @@ __device__ inline uint32_t pair_hi(float a, float b)
     return __builtin_amdgcn_perm(mx_word(a), mx_word(b), 0x07060302u);
 }
 
-// What a lane holds of a step: 8 rows of 4 Words columns, of their scales, and of CT channels.
-template <int CT, int Words>
+// Bytes j and j + 1 (j = 0 or 2) of a word of e4m3 codes, times a scale, as a pair of bfloat16: exact, and NaN
+// for the scale of byte 255 (checked for every code and scale).
+__device__ inline uint32_t scaled_pair(uint32_t codes, float scale, int j)
+{
+    return j == 0 ? __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, false))
+                  : __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(codes, scale, true));
+}
+
+// What a lane holds of a step: 8 rows of 4 Words columns and of Q channels; one word of scales, which its
+// wavefront exchanges.
+template <Num T, int Q, int Words>
 struct Step {
-    uint32_t code[8][Words], scale[8];
-    float g[CT][8];
+    uint32_t code[8][Words], scale;
+    typename NumTraits<T>::type g[8][Q];
     uint32_t live;
 };
 
-// CT tiles of 32 channels by 128 Words columns per wavefront.
-template <Num T, Mx F, int CT, int Words>
+// 16 Q channels by 64 Words columns per wavefront.
+template <Num T, Mx F, int Q, int Words>
 __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
 {
     using E = typename NumTraits<T>::type;
-    constexpr int kCols = 128 * Words;
+    constexpr int kCols = 64 * Words;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-    const int c = lane & 31, h = lane >> 5;
+    const int c = lane & 15, g = lane >> 4;
     const int etile = blockIdx.x, ttile = blockIdx.y, split = blockIdx.z;
 
-    // columns and channels past the end read the last valid ones and are not stored
+    // Columns past the end read the last valid ones and are not stored.  Lane c of an operand stands for
+    // channels first .. first + Q - 1: the last lanes overlap the ones before where Q does not divide T.
     const uint32_t col = min((uint32_t)(etile * kCols + 4 * Words * c), a.code_pitch - 4 * Words);
     const uint32_t block = col / kMxBlock, shift = 8 * (block & 3);
-    uint32_t code_at[8], grad_at[8], chan[CT];
-    const uint32_t scale_at = 8 * h * a.scale_pitch + (block & ~3u);
+    auto first_channel = [&](int lane16) { return min((ttile * 16 + lane16) * Q, a.T - Q); };
+    const uint32_t first = (uint32_t)first_channel(c);
+    uint32_t code_at[8], grad_at[8];
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
-        code_at[i] = (8 * h + i) * a.code_pitch + col;
-        grad_at[i] = (8 * h + i) * a.grad_stride;
+        const uint32_t row = min((uint32_t)(8 * g + i), a.M - 1);
+        code_at[i] = row * a.code_pitch + col;
+        grad_at[i] = row * a.grad_stride + first;
     }
-#pragma unroll
-    for (int q = 0; q < CT; ++q) chan[q] = (uint32_t)min((ttile * CT + q) * kChanTile + c, a.T - 1);
+    // lane l fetches scale word l / 32 of the tile's columns of row l % 32; lane (c, g) needs that of its
+    // column in rows 8 g + i
+    const uint32_t word0 = etile * kCols / (4 * kMxBlock), word = word0 + (Words == 4 ? lane >> 5 : 0);
+    const uint32_t scale_at = min((uint32_t)(lane & 31), a.M - 1) * a.scale_pitch + min(4 * word, a.scale_pitch - 4);
+    const int scale_from = 4 * (8 * g + (Words == 4 ? 32 * (int)((block >> 2) - word0) : 0));
 
     const uint32_t s0 = (uint32_t)split * a.steps_per_split;
     const uint32_t s1 = min(s0 + a.steps_per_split, a.steps);
@@ -94,73 +111,76 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
     auto mask = [&](uint32_t step) -> uint32_t {
         if (step >= s1) return 0u;
         const uint32_t m0 = step * kRows;
-        if (!a.natoms) return a.M - m0 >= kRows ? 0xffffu : (1u << (a.M - m0)) - 1u;
-        const uint32_t m = m0 + (lane & 15), mc = min(m, a.M - 1);
-        const uint32_t b = (__umulhi(mc, a.div_mul) + mc) >> a.div_shift;
-        return (uint32_t)__ballot(m < a.M && (int)(mc - b * a.N) < a.natoms[b]) & 0xffffu;
+        const uint32_t rows = min(a.M - m0, (uint32_t)kRows);
+        if (!a.natoms) return 0xffffffffu >> (kRows - rows);
+        uint32_t b = (__umulhi(m0, a.div_mul) + m0) >> a.div_shift, from = m0 - b * a.N, live = 0;
+        for (uint32_t done = 0; done < rows; ++b, from = 0) {
+            const uint32_t run = min(a.N - from, rows - done);      // of example b
+            const int left = min(max(a.natoms[b] - (int)from, 0), (int)run);
+            if (left > 0) live |= (0xffffffffu >> (kRows - left)) << done;
+            done += run;
+        }
+        return live;
     };
-    auto load = [&](uint32_t step, uint32_t live, Step<CT, Words> &r) {
-        r.live = live;
-        if (live == 0) return;
-        const uint32_t m0 = step * kRows;
+    // No branch lies around the loads: the compiler counts those under way, and where their number depends on
+    // the path it waits for all of them.  The last step takes the last 32 rows (its mask says which are new),
+    // a step without live rows takes the workgroup's first rows again, which are near.
+    const uint32_t most = a.M > kRows ? a.M - kRows : 0u;
+    auto load = [&](uint32_t step, uint32_t live, Step<T, Q, Words> &r) {
+        const uint32_t want = (live ? step : s0) * kRows, m0 = min(want, most);
+        r.live = live ? live << (want - m0) : 0u;
         const uint8_t *cb = a.codes + (int64_t)m0 * a.code_pitch;
         const uint8_t *sb = a.scales + (int64_t)m0 * a.scale_pitch;
         const E *gb = (const E *)a.grad + (int64_t)m0 * a.grad_stride;
-        auto get = [&](int i, uint32_t ca, uint32_t sa, uint32_t ga) {
-            __builtin_memcpy(r.code[i], __builtin_assume_aligned(cb + ca, 4 * Words), 4 * Words);
-            r.scale[i] = *(const uint32_t *)(sb + sa);
+        r.scale = *(const uint32_t *)(sb + scale_at);
 #pragma unroll
-            for (int q = 0; q < CT; ++q) r.g[q][i] = (float)gb[ga + chan[q]];
-        };
-        if (a.M - m0 >= kRows) {
-#pragma unroll
-            for (int i = 0; i < 8; ++i) get(i, code_at[i], scale_at + i * a.scale_pitch, grad_at[i]);
-        } else {                            // the last step: rows past the end read the last row
-            const uint32_t last = a.M - 1 - m0;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                const uint32_t over = max((uint32_t)(8 * h + i), last) - last;
-                get(i, code_at[i] - over * a.code_pitch, scale_at + i * a.scale_pitch - over * a.scale_pitch,
-                    grad_at[i] - over * a.grad_stride);
-            }
+        for (int i = 0; i < 8; ++i) {
+            __builtin_memcpy(r.code[i], __builtin_assume_aligned(cb + code_at[i], 4 * Words), 4 * Words);
+            __builtin_memcpy(r.g[i], gb + grad_at[i], sizeof r.g[i]);
         }
     };
 
-    v16f acc[CT][Words][4];
+    v4f acc[Q][Words][4];
 #pragma unroll
-    for (int q = 0; q < CT; ++q)
+    for (int q = 0; q < Q; ++q)
 #pragma unroll
         for (int w = 0; w < Words; ++w)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
+            for (int j = 0; j < 4; ++j) acc[q][w][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+    float bias[Q];
 #pragma unroll
-                for (int i = 0; i < 16; ++i) acc[q][w][j][i] = 0.0f;
-    float bias[CT];
-#pragma unroll
-    for (int q = 0; q < CT; ++q) bias[q] = 0.0f;
+    for (int q = 0; q < Q; ++q) bias[q] = 0.0f;
 
-    auto compute = [&](Step<CT, Words> &r) {
+    auto compute = [&](Step<T, Q, Words> &r) {
         if (r.live == 0) return;
-        if (r.live != 0xffffu) {
-            const uint32_t mine = r.live >> (8 * h);
+        float s[8], off[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const uint32_t w = (uint32_t)__builtin_amdgcn_ds_bpermute(scale_from + 4 * i, (int)r.scale);
+            s[i] = mx_bits(((w >> shift) & 255u) << 23);        // S = 255: infinity, times code 0
+        }
+        if (r.live != 0xffffffffu) {
+            const uint32_t mine = r.live >> (8 * g);
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
                 const bool on = (mine >> i) & 1u;
-                r.scale[i] = on ? r.scale[i] : 0u;          // times code 0: e4m3 codes can be NaN
+                s[i] = on ? s[i] : 0.0f;                        // times code 0: e4m3 codes can be NaN
 #pragma unroll
                 for (int w = 0; w < Words; ++w) r.code[i][w] = on ? r.code[i][w] : 0u;
 #pragma unroll
-                for (int q = 0; q < CT; ++q) r.g[q][i] = on ? r.g[q][i] : 0.0f;
+                for (int q = 0; q < Q; ++q) r.g[i][q] = on ? r.g[i][q] : (E)0.0f;
             }
         }
-        v8bf gp[CT][kPieces<T>];
 #pragma unroll
-        for (int q = 0; q < CT; ++q) {
+        for (int i = 0; i < 8; ++i) off[i] = -128.0f * s[i];
+        v8bf gp[Q][kPieces<T>];
+#pragma unroll
+        for (int q = 0; q < Q; ++q) {
             float rest[8];
 #pragma unroll
             for (int i = 0; i < 8; ++i) {
-                rest[i] = r.g[q][i];
-                bias[q] += rest[i];
+                rest[i] = (float)r.g[i][q];
+                if (etile == 0) bias[q] += rest[i];
             }
 #pragma unroll
             for (int p = 0; p < kPieces<T>; ++p) {
@@ -173,119 +193,114 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
                 }
             }
         }
-        float s[8], off[8];
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-            s[i] = mx_bits(((r.scale[i] >> shift) & 255u) << 23);       // S = 255: infinity, times code 0
-            off[i] = -128.0f * s[i];
-        }
 #pragma unroll
         for (int w = 0; w < Words; ++w) {
             // this lane's 8 rows of 4 columns, as 4 operands
-            float x[4][8];
+            v4u x[4];
+            if constexpr (F == Mx::INT8) {
+                // bytes as q + 128, which one conversion takes; (q + 128) s - 128 s = q s is exact
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                if constexpr (F == Mx::INT8) {
-                    // bytes as q + 128, which one conversion takes; (q + 128) s - 128 s = q s is exact
-                    const uint32_t u = r.code[i][w] ^ 0x80808080u;
+                for (int i = 0; i < 8; i += 2) {
+                    const uint32_t u = r.code[i][w] ^ 0x80808080u, v = r.code[i + 1][w] ^ 0x80808080u;
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) x[j][i] = fmaf((float)((u >> (8 * j)) & 255u), s[i], off[i]);
-                } else {
-                    const auto lo = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.code[i][w], false);
-                    const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.code[i][w], true);
-                    x[0][i] = lo[0] * s[i];
-                    x[1][i] = lo[1] * s[i];
-                    x[2][i] = hi[0] * s[i];
-                    x[3][i] = hi[1] * s[i];
+                    for (int j = 0; j < 4; ++j)
+                        x[j][i / 2] = pair_hi(fmaf((float)((v >> (8 * j)) & 255u), s[i + 1], off[i + 1]),
+                                              fmaf((float)((u >> (8 * j)) & 255u), s[i], off[i]));
                 }
+            } else {
+                // two columns of a row at a time, then two rows of each
+#pragma unroll
+                for (int i = 0; i < 8; i += 2)
+#pragma unroll
+                    for (int j = 0; j < 4; j += 2) {
+                        const uint32_t u = scaled_pair(r.code[i][w], s[i], j), v = scaled_pair(r.code[i + 1][w], s[i + 1], j);
+                        x[j][i / 2] = __builtin_amdgcn_perm(v, u, 0x05040100u);
+                        x[j + 1][i / 2] = __builtin_amdgcn_perm(v, u, 0x07060302u);
+                    }
             }
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                const v4u v = {pair_hi(x[j][1], x[j][0]), pair_hi(x[j][3], x[j][2]), pair_hi(x[j][5], x[j][4]),
-                               pair_hi(x[j][7], x[j][6])};
-                const v8bf xb = __builtin_bit_cast(v8bf, v);
+                const v8bf xb = __builtin_bit_cast(v8bf, x[j]);
 #pragma unroll
-                for (int q = 0; q < CT; ++q)
+                for (int q = 0; q < Q; ++q)
 #pragma unroll
                     for (int p = 0; p < kPieces<T>; ++p)
-                        acc[q][w][j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(gp[q][p], xb, acc[q][w][j], 0, 0, 0);
+                        acc[q][w][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(gp[q][p], xb, acc[q][w][j], 0, 0, 0);
             }
         }
     };
 
+    Step<T, Q, Words> ring[kDepth];
+    uint32_t ahead = mask(s0 + wave);
     {
-        uint32_t step = s0 + wave;
-        uint32_t live = mask(step), ahead = mask(step + kWaves);
-        Step<CT, Words> now, next;
-        load(step, live, now);
-        for (; step < s1; step += kWaves) {
-            load(step + kWaves, ahead, next);
-            ahead = mask(step + 2 * kWaves);
-            compute(now);
-            now = next;
+#pragma unroll
+        for (int d = 0; d < kDepth - 1; ++d) {
+            const uint32_t step = s0 + wave + d * kWaves, live = ahead;
+            ahead = mask(step + kWaves);
+            load(step, live, ring[d]);
+        }
+        for (uint32_t step0 = s0 + wave;; step0 += kDepth * kWaves) {
+#pragma unroll
+            for (int d = 0; d < kDepth; ++d) {
+                const uint32_t step = step0 + d * kWaves, live = ahead;
+                if (step >= s1) goto done;
+                ahead = mask(step + kDepth * kWaves);
+                load(step + (kDepth - 1) * kWaves, live, ring[(d + kDepth - 1) % kDepth]);
+                compute(ring[d]);
+            }
         }
     }
+done:
 
-    // The wavefronts' sums, one tile of 32 channels by 128 columns at a time, through LDS as [wavefront]
-    // [accumulator row][lane] of 4 columns: the upper four hand theirs to the lower four, those lay out
-    // theirs, and every wavefront adds up and stores two accumulator rows.
-    __shared__ float4 sums[kWaves / 2][16][64];
-    __shared__ float bsum[kWaves][32];
+    // The wavefronts' sums, 16 of a lane's channels at a time, through LDS as [wavefront][item][lane] of 4
+    // columns, an item being one of a lane's four accumulator rows and one of its words; the wavefronts share
+    // the items out, add them up and store them.
+    constexpr int kItems = 4 * Words;
+    __shared__ float4 sums[kWaves][kItems][64];
+    __shared__ float bsum[kWaves][16];
     const int64_t weights = (int64_t)a.T * a.code_pitch;
 #pragma unroll
-    for (int q = 0; q < CT; ++q) {
-        const int t0 = (ttile * CT + q) * kChanTile;
-        const float b = bias[q] + __shfl_xor(bias[q], 32);
+    for (int q = 0; q < Q; ++q) {
         if (q) __syncthreads();
-        if (h == 0) bsum[wave][c] = b;
+        float b = bias[q];
+        b += __shfl_xor(b, 16);
+        b += __shfl_xor(b, 32);
+        if (g == 0) bsum[wave][c] = b;
 #pragma unroll
-        for (int w = 0; w < Words; ++w) {
-            if (w) __syncthreads();
-            if (wave >= kWaves / 2) {
+        for (int i = 0; i < 4; ++i)
 #pragma unroll
-                for (int i = 0; i < 16; ++i)
-                    sums[wave - kWaves / 2][i][lane] =
-                        make_float4(acc[q][w][0][i], acc[q][w][1][i], acc[q][w][2][i], acc[q][w][3][i]);
-            }
-            __syncthreads();
-            if (wave < kWaves / 2) {
-#pragma unroll
-                for (int i = 0; i < 16; ++i) {
-                    const float4 o = sums[wave][i][lane];
-                    sums[wave][i][lane] = make_float4(acc[q][w][0][i] + o.x, acc[q][w][1][i] + o.y,
-                                                      acc[q][w][2][i] + o.z, acc[q][w][3][i] + o.w);
-                }
-            }
-            __syncthreads();
-            if (w == 0 && etile == 0 && threadIdx.x < 32 && t0 + (int)threadIdx.x < a.T) {
-                const int t = t0 + threadIdx.x;
+            for (int w = 0; w < Words; ++w)
+                sums[wave][i * Words + w][lane] =
+                    make_float4(acc[q][w][0][i], acc[q][w][1][i], acc[q][w][2][i], acc[q][w][3][i]);
+        __syncthreads();
+        if (etile == 0 && threadIdx.x < 16) {
+            const int own = (ttile * 16 + (int)threadIdx.x) * Q, t = first_channel(threadIdx.x) + q;
+            if (t >= own && own < a.T) {
                 float v = 0.0f;
 #pragma unroll
-                for (int k = 0; k < kWaves; ++k) v += bsum[k][threadIdx.x];
+                for (int o = 0; o < kWaves; ++o) v += bsum[o][threadIdx.x];
                 if (a.splits > 1) a.partial[(int64_t)a.splits * weights + (int64_t)split * a.T + t] = v;
                 else if (a.bias) a.bias[t] = v;
             }
+        }
+        for (int item = wave; item < kItems; item += kWaves) {
+            const int row = 4 * g + item / Words, own = (ttile * 16 + row) * Q, t = first_channel(row) + q;
+            const int e = etile * kCols + 4 * Words * c + 4 * (item % Words);
+            if (t < own || own >= a.T || e >= a.E) continue;    // a channel is stored by the first lane that has it
+            float4 v = sums[0][item][lane];
 #pragma unroll
-            for (int k = 0; k < 16 / kWaves; ++k) {
-                const int i = 16 / kWaves * wave + k;
-                const int t = t0 + 8 * (i >> 2) + 4 * h + (i & 3);
-                const int e = etile * kCols + 4 * Words * c + 4 * w;
-                float4 v = sums[0][i][lane];
-#pragma unroll
-                for (int o = 1; o < kWaves / 2; ++o) {
-                    const float4 x = sums[o][i][lane];
-                    v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
-                }
-                if (t >= a.T || e >= a.E) continue;
-                if (a.splits == 1) {
-                    float *to = a.weight + (int64_t)t * a.E + e;
-                    to[0] = v.x;
-                    if (e + 1 < a.E) to[1] = v.y;
-                    if (e + 2 < a.E) to[2] = v.z;
-                    if (e + 3 < a.E) to[3] = v.w;
-                } else {
-                    *(float4 *)(a.partial + (int64_t)split * weights + (int64_t)t * a.code_pitch + e) = v;
-                }
+            for (int o = 1; o < kWaves; ++o) {
+                const float4 x = sums[o][item][lane];
+                v.x += x.x; v.y += x.y; v.z += x.z; v.w += x.w;
+            }
+            if (a.splits == 1) {
+                float *to = a.weight + (int64_t)t * a.E + e;
+                to[0] = v.x;
+                if (e + 1 < a.E) to[1] = v.y;
+                if (e + 2 < a.E) to[2] = v.z;
+                if (e + 3 < a.E) to[3] = v.w;
+            } else {
+                *(float4 *)(a.partial + (int64_t)split * weights + (int64_t)t * a.code_pitch + e) = v;
             }
         }
     }
@@ -339,35 +354,32 @@ __global__ __launch_bounds__(kSumThreads) void gradient_sum_kernel(GradientArgs 
     if (e + 3 < a.E) to[3] = v.w;
 }
 
-// Two tiles of channels share a pass over the codes where there are that many channels; else a wavefront
-// takes 256 columns, so that it meets the gradients half as often.
-int channel_tiles(int64_t T) { return T > kChanTile ? 2 : 1; }
-int column_words(int64_t T, int64_t pitch) { return T <= kChanTile && pitch > 128 ? 2 : 1; }
+// Channels a lane takes (of the gradient, in one load) and words of codes.
+int lane_channels(int64_t T) { return T > 16 ? 2 : 1; }
+int lane_words(int64_t T, int64_t pitch) { return T > 16 ? 2 : pitch > 64 ? 4 : 1; }
 
 int64_t gradient_tiles(int64_t T, int64_t pitch)
 {
-    const int64_t cols = 128 * column_words(T, pitch), chans = kChanTile * channel_tiles(T);
+    const int64_t cols = 64 * lane_words(T, pitch), chans = 16 * lane_channels(T);
     return ((pitch + cols - 1) / cols) * ((T + chans - 1) / chans);
 }
 
-// Enough workgroups to fill the chip, but at least kLeastSteps steps of 16 rows per wavefront, as every split
-// costs a write and a read of T x E sums.
-constexpr int kWantGroups = 256, kLeastSteps = 2;
+// Enough workgroups to fill the chip, but at least a step of 32 rows per wavefront, as every split costs a
+// write and a read of T x E sums.
+constexpr int kWantGroups = 256;
 int gradient_splits(int64_t M, int64_t T, int64_t E)
 {
     const int64_t steps = (M + kRows - 1) / kRows;
     const int64_t tiles = gradient_tiles(T, mx_blocks(E) * kMxBlock);
-    const int64_t want = (kWantGroups + tiles - 1) / tiles;
-    const int64_t most = (steps + kLeastSteps * kWaves - 1) / (kLeastSteps * kWaves);
+    const int64_t want = (kWantGroups + tiles - 1) / tiles, most = (steps + kWaves - 1) / kWaves;
     return (int)std::max<int64_t>(1, std::min(want, most));
 }
 
-template <Num T, Mx F, int CT, int Words>
+template <Num T, Mx F, int Q, int Words>
 hipError_t gradient_run(const GradientArgs &a, hipStream_t stream)
 {
-    const dim3 grid((a.code_pitch + 128 * Words - 1) / (128 * Words), (a.T + kChanTile * CT - 1) / (kChanTile * CT),
-                    a.splits);
-    hipLaunchKernelGGL((gradient_kernel<T, F, CT, Words>), grid, dim3(kThreads), 0, stream, a);
+    const dim3 grid((a.code_pitch + 64 * Words - 1) / (64 * Words), (a.T + 16 * Q - 1) / (16 * Q), a.splits);
+    hipLaunchKernelGGL((gradient_kernel<T, F, Q, Words>), grid, dim3(kThreads), 0, stream, a);
     if (a.splits > 1) {
         const dim3 sum((a.code_pitch + 127) / 128 + 1, a.T);
         hipLaunchKernelGGL(gradient_sum_kernel, sum, dim3(kSumThreads), 0, stream, a);
@@ -378,9 +390,9 @@ hipError_t gradient_run(const GradientArgs &a, hipStream_t stream)
 template <Num T, Mx F>
 hipError_t gradient_typed(const GradientArgs &a, hipStream_t stream)
 {
-    if (channel_tiles(a.T) == 2) return gradient_run<T, F, 2, 1>(a, stream);
-    if (column_words(a.T, a.code_pitch) == 2) return gradient_run<T, F, 1, 2>(a, stream);
-    return gradient_run<T, F, 1, 1>(a, stream);
+    const int words = lane_words(a.T, a.code_pitch);
+    if (lane_channels(a.T) == 2) return gradient_run<T, F, 2, 2>(a, stream);
+    return words == 4 ? gradient_run<T, F, 1, 4>(a, stream) : gradient_run<T, F, 1, 1>(a, stream);
 }
 
 }  // namespace
