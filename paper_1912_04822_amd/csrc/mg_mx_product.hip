@@ -148,10 +148,12 @@ __device__ inline void store_results(const ProductArgs &p, int m, int n, v4f v)
 }
 
 // Operands straight from memory.  A wavefront holds RM x RN tiles of 16 x 16; the KW wavefronts of a
-// group share a tile and split k between them (their sums meet in LDS), the others lie along m.
+// group share a tile and split k between them (their sums meet in LDS), the others lie along m.  Two steps'
+// operands are asked for at a time.
 template <Num T, bool Plain, int RM, int RN, int Waves, int KW>
 __global__ __launch_bounds__(64 * Waves) void product_kernel(ProductArgs p)
 {
+    constexpr int U = 2;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int r = lane & 15, g = lane >> 4;
     const int kw = wave % KW, mw = wave / KW;
@@ -169,41 +171,49 @@ __global__ __launch_bounds__(64 * Waves) void product_kernel(ProductArgs p)
 #pragma unroll
     for (int j = 0; j < RN; ++j) brow[j] = min(n0 + 16 * j + r, p.N - 1);
 
-    for (int k = kw * 4; k < p.blocks; k += KW * 4) {
-        Operand a[RM], b[RN];
+    for (int k = kw * 4; k < p.blocks; k += U * KW * 4) {
+        Operand a[U][RM], b[U][RN];
 #pragma unroll
-        for (int i = 0; i < RM; ++i) {
-            if constexpr (Plain) a[i] = quantise_block<T>(p, arow[i], k + g);
-            else a[i] = load_block((const uint8_t *)p.a, p.a_scales, p, arow[i], k + g);
-        }
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-        for (int j = 0; j < RN; ++j) b[j] = load_block(p.b, p.b_scales, p, brow[j], k + g);
+            for (int j = 0; j < RN; ++j) b[u][j] = load_block(p.b, p.b_scales, p, brow[j], k + u * KW * 4 + g);
 #pragma unroll
-        for (int i = 0; i < RM; ++i)
+        for (int u = 0; u < U; ++u)
 #pragma unroll
-            for (int j = 0; j < RN; ++j) acc[i][j] = product(b[j], a[i], acc[i][j]);
+            for (int i = 0; i < RM; ++i) {
+                if constexpr (Plain) a[u][i] = quantise_block<T>(p, arow[i], k + u * KW * 4 + g);
+                else a[u][i] = load_block((const uint8_t *)p.a, p.a_scales, p, arow[i], k + u * KW * 4 + g);
+            }
+#pragma unroll
+        for (int u = 0; u < U; ++u)
+#pragma unroll
+            for (int i = 0; i < RM; ++i)
+#pragma unroll
+                for (int j = 0; j < RN; ++j) acc[i][j] = product(b[u][j], a[u][i], acc[i][j]);
     }
 
     if constexpr (KW > 1) {
+        // the sums of a group in LDS; every wavefront of it adds up and stores its share of the tiles
         __shared__ v4f sums[Waves][RM * RN][64];
 #pragma unroll
         for (int i = 0; i < RM; ++i)
 #pragma unroll
             for (int j = 0; j < RN; ++j) sums[wave][i * RN + j][lane] = acc[i][j];
         __syncthreads();
-        if (kw != 0) return;
+        for (int tile = kw; tile < RM * RN; tile += KW) {
+            v4f v = sums[mw * KW][tile][lane];
 #pragma unroll
-        for (int i = 0; i < RM; ++i)
+            for (int w = 1; w < KW; ++w) v += sums[mw * KW + w][tile][lane];
+            const int n = n0 + 16 * (tile % RN) + 4 * g;
+            store_results<T>(p, m0 + 16 * (tile / RN) + r, n, v + load_bias(p, n));
+        }
+    } else {
 #pragma unroll
-            for (int j = 0; j < RN; ++j)
+        for (int j = 0; j < RN; ++j) {
+            const v4f bias = load_bias(p, n0 + 16 * j + 4 * g);
 #pragma unroll
-                for (int w = 1; w < KW; ++w) acc[i][j] += sums[wave + w][i * RN + j][lane];
-    }
-#pragma unroll
-    for (int j = 0; j < RN; ++j) {
-        const v4f bias = load_bias(p, n0 + 16 * j + 4 * g);
-#pragma unroll
-        for (int i = 0; i < RM; ++i) store_results<T>(p, m0 + 16 * i + r, n0 + 16 * j + 4 * g, acc[i][j] + bias);
+            for (int i = 0; i < RM; ++i) store_results<T>(p, m0 + 16 * i + r, n0 + 16 * j + 4 * g, acc[i][j] + bias);
+        }
     }
 }
 
@@ -216,12 +226,13 @@ hipError_t direct(const ProductArgs &p, hipStream_t stream)
     return hipGetLastError();
 }
 
-// Large products: a workgroup of 4 wavefronts makes a 256 x 256 tile of C, each wavefront 128 x 128 of it
-// (4 x 4 tiles of 32 x 32 in 256 accumulator registers, one wavefront per SIMD) with
-// v_mfma_scale_f32_32x32x64_f8f6f4: from registers alone it reaches 9.0 PFLOP/s (6.3 with random codes, where
-// the chip lowers its clock), the 16 x 16 x 128 form 5.6 (4.9).  Codes go through LDS, where every byte is
-// read by two wavefronts: per 128 k a wavefront issues 32 products (1024 cycles of its matrix core) for 16
-// operands of 1 KB.
+// Large products: a workgroup of 4 wavefronts makes a square tile of C, each wavefront a quarter of it as WT x WT
+// tiles of 32 x 32, with v_mfma_scale_f32_32x32x64_f8f6f4: from registers alone it reaches 9.0 PFLOP/s (6.3 with
+// random codes, where the chip lowers its clock), the 16 x 16 x 128 form 5.6 (4.9).  Codes go through LDS, where
+// every byte is read by two wavefronts.  WT = 4, 256 x 256 in 256 accumulator registers, one wavefront per SIMD:
+// per 128 k a wavefront issues 32 products (1024 cycles of its matrix core) for 16 operands of 1 KB.  WT = 2,
+// 128 x 128, two workgroups to a compute unit: twice the reads of LDS per product, for products that are too
+// small to fill the chip with large tiles.
 //   - Four buffers of 128 k.  Codes go from memory to LDS without passing registers, four steps ahead, and
 //     from LDS to registers one step ahead, while the products of the step before run: neither is waited for
 //     in steady state.  A wavefront waits for its own loads of the next step only, then for the others at the
@@ -233,7 +244,6 @@ hipError_t direct(const ProductArgs &p, hipStream_t stream)
 //     instruction picks by its operand selector.
 // Past the end of k the codes of A are zeros and the scales powers of two; rows past M or N repeat the last
 // one and are not stored.
-constexpr int kTile = 256;
 
 __device__ inline uint32_t tile_place(uint32_t row, uint32_t piece) { return row * 4 + (piece ^ ((row >> 2) & 3)); }
 
@@ -272,12 +282,14 @@ template <int N> __device__ inline void wait_loads()
     __builtin_amdgcn_s_waitcnt((N & 15) | (7 << 4) | (N >> 4) << 14);
 }
 
-template <Num T>
-__global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int mtiles, int ntiles)
+template <Num T, int WT>
+__global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(ProductArgs p, int mtiles, int ntiles)
 {
+    constexpr int kTile = 64 * WT;
     constexpr int kBuffer = kTile * 8;                      // 16-byte pieces of a buffer: codes of A, then of B
+    constexpr int kLoads = 2 * WT;                          // a wavefront's loads of a step, 16 rows each
     __shared__ v4u lds[4 * kBuffer + 2 * kTile];            // then 16 bytes of scales for every row of A and B
-    v4u *const lds_sa = lds + 4 * kBuffer, *const lds_sb = lds_sa + kTile;
+    v4u *const lds_s = lds + 4 * kBuffer;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5;                 // an operand: row r, the h-th 32 of its 64 k
     const int wm = wave >> 1, wn = wave & 1;
@@ -297,72 +309,68 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
     const uint8_t *const base_a = (const uint8_t *)p.a + (int64_t)m0 * p.pitch;
     const uint8_t *const base_b = p.b + (int64_t)n0 * p.pitch;
     const uint32_t piece = (lane & 3) ^ (lane >> 4);        // see tile_place: row / 4 = lane / 16 modulo 4
-    uint32_t off_a[4], off_b[4];
+    uint32_t off[kLoads];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = (4 * i + wave) * 16 + (lane >> 2);
-        off_a[i] = (uint32_t)min(row, p.M - 1 - m0) * p.pitch + 16 * piece;
-        off_b[i] = (uint32_t)min(row, p.N - 1 - n0) * p.pitch + 16 * piece;
+    for (int i = 0; i < kLoads; ++i) {
+        const int row = (4 * (i % WT) + wave) * 16 + (lane >> 2);
+        off[i] = (uint32_t)min(row, (i < WT ? p.M - m0 : p.N - n0) - 1) * p.pitch + 16 * piece;
     }
     const uint32_t put = lds_address(lds) + wave * 1024;
-    // one of the eight loads of a step: 16 rows of A (0 .. 3) or B per wavefront
-    auto fetch = [&](int step, int buffer, int which, uint32_t back) {
-        const uint32_t to = put + (buffer * kBuffer + which * kTile) * 16;
-        if (which < 4) load_to_lds(base_a + step * 64, off_a[which] - back, to);
-        else load_to_lds(base_b + step * 64, off_b[which - 4] - back, to);
+    auto fetch = [&](int step, int buffer, int which, uint32_t back) {      // 16 rows of A, or (from WT on) of B
+        load_to_lds((which < WT ? base_a : base_b) + step * 64, off[which] - back, put + buffer * kBuffer * 16 + which * 4096);
     };
     // pieces past a row's end are not read: the lane takes the step's first piece, which its row has
     auto past_end = [&](int step) { return step * 4 + (int)piece < p.blocks ? 0u : 16 * piece; };
-    const uint32_t scale_off_a = (uint32_t)min(tid, p.M - 1 - m0) * p.scale_pitch;
-    const uint32_t scale_off_b = (uint32_t)min(tid, p.N - 1 - n0) * p.scale_pitch;
-    const uint8_t *const scale_a = p.a_scales + (int64_t)m0 * p.scale_pitch;
-    const uint8_t *const scale_b = p.b_scales + (int64_t)n0 * p.scale_pitch;
-    const uint32_t put_sa = lds_address(lds_sa) + wave * 1024, put_sb = lds_address(lds_sb) + wave * 1024;
     auto fetch_scales = [&](int step) {                     // of steps step .. step + 3
-        if (step * 4 + 16 <= p.blocks) {
-            load_to_lds(scale_a + step * 4, scale_off_a, put_sa);
-            load_to_lds(scale_b + step * 4, scale_off_b, put_sb);
-            return;
-        }
-        v4u sa, sb;                                         // a row's end: bytes past it become zeros
 #pragma unroll
-        for (int w = 0; w < 4; ++w) {
-            const int left = p.blocks - (step + w) * 4;     // blocks of this word
-            const uint32_t mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
-            sa[w] = left > 0 ? *(const uint32_t *)(scale_a + scale_off_a + (step + w) * 4) & mask : 0u;
-            sb[w] = left > 0 ? *(const uint32_t *)(scale_b + scale_off_b + (step + w) * 4) & mask : 0u;
+        for (int i = 0; i < WT / 2; ++i) {
+            const int unit = 4 * i + wave;                  // 64 rows of A, or (from WT on) of B
+            const bool of_b = unit >= WT;
+            const uint8_t *base = of_b ? p.b_scales + (int64_t)n0 * p.scale_pitch : p.a_scales + (int64_t)m0 * p.scale_pitch;
+            const int row = (of_b ? unit - WT : unit) * 64 + lane;
+            const uint32_t at = (uint32_t)min(row, (of_b ? p.N - n0 : p.M - m0) - 1) * p.scale_pitch;
+            if (step * 4 + 16 <= p.blocks) {
+                load_to_lds(base + step * 4, at, lds_address(lds_s) + unit * 1024);
+                continue;
+            }
+            v4u s;                                          // a row's end: bytes past it become zeros
+#pragma unroll
+            for (int w = 0; w < 4; ++w) {
+                const int left = p.blocks - (step + w) * 4; // blocks of this word
+                const uint32_t mask = left >= 4 ? 0xffffffffu : left <= 0 ? 0u : (1u << (8 * left)) - 1u;
+                s[w] = left > 0 ? *(const uint32_t *)(base + at + (step + w) * 4) & mask : 0u;
+            }
+            lds_s[unit * 64 + lane] = s;
         }
-        lds_sa[tid] = sa;
-        lds_sb[tid] = sb;
     };
 
     const uint32_t lane_at[2] = {tile_place(r, h), tile_place(r, 2 + h)};       // first and second 64 k
     struct Operands {
-        v4u a[2][4], b[2][4];
+        v4u a[2][WT], b[2][WT];
     };
-    auto read = [&](int buffer, int which, Operands &o) {   // one of sixteen
+    auto read = [&](int buffer, int which, Operands &o) {   // one of 4 WT, those of the first 64 k first
         const v4u *from = lds + buffer * kBuffer;
-        const int k = which >> 3, i = which & 3;
-        if (which & 4) o.a[k][i] = from[(wm * 4 + i) * 128 + lane_at[k]];
-        else o.b[k][i] = from[kTile * 4 + (wn * 4 + i) * 128 + lane_at[k]];
+        const int k = which / (2 * WT), i = which % WT;
+        if (which / WT & 1) o.a[k][i] = from[(wm * WT + i) * 128 + lane_at[k]];
+        else o.b[k][i] = from[kTile * 4 + (wn * WT + i) * 128 + lane_at[k]];
     };
     const uint32_t pick = (uint32_t)h | (uint32_t)(4 + h) << 8 | 0x0c0c0000u;
     struct Scales {
-        int a[2][4], b[2][4];
+        int a[2][WT], b[2][WT];
     };
-    auto read_scales = [&](int i, Scales &s) {              // one of the four rows of tiles
-        const v4u a = lds_sa[wm * 128 + 32 * i + r], b = lds_sb[wn * 128 + 32 * i + r];
+    auto read_scales = [&](int i, Scales &s) {              // one of the WT rows of tiles
+        const v4u a = lds_s[(wm * WT + i) * 32 + r], b = lds_s[kTile + (wn * WT + i) * 32 + r];
         s.a[0][i] = scale_bytes(a, pick);
         s.b[0][i] = scale_bytes(b, pick);
         s.a[1][i] = scale_bytes(a, pick + 0x0202u);
         s.b[1][i] = scale_bytes(b, pick + 0x0202u);
     };
 
-    v16f acc[4][4];
+    v16f acc[WT][WT];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
+    for (int i = 0; i < WT; ++i)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < WT; ++j)
 #pragma unroll
             for (int q = 0; q < 16; ++q) acc[i][j][q] = 0.0f;
 
@@ -374,15 +382,15 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
         if (s < steps) {
             const uint32_t back = past_end(s);
 #pragma unroll
-            for (int q = 0; q < 8; ++q) fetch(s, s, q, back);
+            for (int q = 0; q < kLoads; ++q) fetch(s, s, q, back);
         }
-    if (steps > 3) wait_loads<24>();
+    if (steps > 3) wait_loads<3 * kLoads>();
     else wait_loads<0>();
     __builtin_amdgcn_s_barrier();
 #pragma unroll
-    for (int q = 0; q < 16; ++q) read(0, q, even);
+    for (int q = 0; q < 4 * WT; ++q) read(0, q, even);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) read_scales(i, later);
+    for (int i = 0; i < WT; ++i) read_scales(i, later);
 
     for (int step0 = 0; step0 < steps; step0 += 4) {
         scales = later;
@@ -396,7 +404,7 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
             const int step = step0 + W;
             if (step >= steps) return;
             Operands &now = W & 1 ? odd : even, &next = W & 1 ? even : odd;
-            wait_loads<16>();
+            wait_loads<2 * kLoads>();
             __builtin_amdgcn_s_barrier();
             if (W == 0 && step + 4 < steps) fetch_scales(step + 4);
             const int ahead = min(step + 4, steps - 1);
@@ -406,17 +414,24 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
                 for (int k = 0; k < 2; ++k) {
                     const bool in_row = step * 4 + 2 * k + h < p.blocks;
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) now.a[k][i] = in_row ? now.a[k][i] : v4u{0, 0, 0, 0};
+                    for (int i = 0; i < WT; ++i) now.a[k][i] = in_row ? now.a[k][i] : v4u{0, 0, 0, 0};
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
+            constexpr int kProducts = 2 * WT * WT, kReads = 4 * WT;
 #pragma unroll
-            for (int t = 0; t < 32; ++t) {
-                const int k = t >> 4, i = (t >> 2) & 3, j = t & 3;
+            for (int t = 0; t < kProducts; ++t) {
+                const int k = t / (WT * WT), i = t / WT % WT, j = t % WT;
                 acc[i][j] = product_step<W>(now.b[k][j], now.a[k][i], acc[i][j], scales.b[k][j], scales.a[k][i]);
-                if (t < 16) read((W + 1) & 3, t, next);
-                if (t >= 16 && (t & 1) == 0) fetch(ahead, W, (t - 16) >> 1, back);
-                if (W >= 2 && (t == 19 || t == 27)) read_scales((W - 2) * 2 + (t == 27), later);
+                if constexpr (WT == 4) {
+                    if (t < kReads) read((W + 1) & 3, t, next);
+                    if (t >= kReads && (t & 1) == 0) fetch(ahead, W, (t - kReads) >> 1, back);
+                    if (W >= 2 && (t == 19 || t == 27)) read_scales((W - 2) * 2 + (t == 27), later);
+                } else {
+                    read((W + 1) & 3, t, next);
+                    if (t & 1) fetch(ahead, W, t >> 1, back);
+                    if (W >= 2 && t == 6) read_scales(W - 2, later);
+                }
                 __builtin_amdgcn_sched_barrier(0);
             }
         };
@@ -426,28 +441,29 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
         one(std::integral_constant<int, 3>{});
     }
 
-    // A wavefront turns its results through LDS, 32 rows of 128 at a time (rows 16 bytes further apart, so
-    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch.
+    // A wavefront turns its results through LDS, 32 rows of 32 WT at a time (rows 16 bytes further apart, so
+    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch.  Kept short: a small
+    // product runs through this code once, and waits for it to come from memory.
     using E = typename NumTraits<T>::type;
-    constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 128 / P, kPitch = 132;
+    constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kPitch = 32 * WT + 4;
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     float *const mine = (float *)(lds + wave * kBuffer);
-    const int col = P * (lane % kLanes), n = n0 + wn * 128 + col;
+    const int col = P * (lane % kLanes), n = n0 + wn * 32 * WT + col;
     float bias[P];
 #pragma unroll
     for (int e = 0; e < P; ++e) bias[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < WT; ++i) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
+        for (int j = 0; j < WT; ++j)
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
                 const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
                 *(v4f *)(mine + r * kPitch + 32 * j + 8 * q + 4 * h) = v;
             }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll
+#pragma unroll 2
         for (int t = 0; t < 32 * kLanes / 64; ++t) {
             const int row = t * (64 / kLanes) + lane / kLanes;
             const float *from = mine + row * kPitch + col;
@@ -458,7 +474,7 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
 #pragma unroll
                 for (int d = 0; d < 4; ++d) e[c + d] = (E)(v[d] + bias[c + d]);
             }
-            const int m = m0 + wm * 128 + 32 * i + row;
+            const int m = m0 + (wm * WT + i) * 32 + row;
             if (m >= p.M) continue;
             E *to = (E *)p.c + (int64_t)m * p.c_stride + n;
             if (n + P <= p.N) {
@@ -473,21 +489,36 @@ __global__ __launch_bounds__(256, 1) void product_tile_kernel(ProductArgs p, int
     }
 }
 
-template <Num T>
+template <Num T, int WT>
 hipError_t tiled(const ProductArgs &p, hipStream_t stream)
 {
-    const int mtiles = (p.M + kTile - 1) / kTile, ntiles = (p.N + kTile - 1) / kTile;
-    hipLaunchKernelGGL((product_tile_kernel<T>), dim3(mtiles * ntiles), dim3(256), 0, stream, p, mtiles, ntiles);
+    const int tile = 64 * WT, mtiles = (p.M + tile - 1) / tile, ntiles = (p.N + tile - 1) / tile;
+    hipLaunchKernelGGL((product_tile_kernel<T, WT>), dim3(mtiles * ntiles), dim3(256), 0, stream, p, mtiles, ntiles);
     return hipGetLastError();
 }
 
+// 16 x 16 tiles of C
+int64_t small_tiles(int M, int N) { return (int64_t)((M + 15) / 16) * ((N + 15) / 16); }
+
+// Which kernel.  Microseconds measured back to back, float results:
+//   - up to 512 tiles of 16 x 16 the chip has room for a workgroup each (1 x 8192 or 300 x 400): a
+//     workgroup per tile, its wavefronts share k.  300 x 300 x 512: 3.4, with 32 x 32 tiles 4.4, 128 x 128 6.7.
+//   - up to 1536, or 4096 where k is one step: 32 x 32 tiles.  8000 x 28 x 2048: 6.4 (16 x 16 9.7, 128 x 128
+//     9.8); 300 x 2048 x 512: 7.9 against 6.9.
+//   - beyond, tiles of 128 or 256 through LDS, by how many rounds of workgroups they take and what a round
+//     costs (us, K in numbers): 14.5 + 0.0075 K for 256 tiles of 256, 8.5 + 0.0052 K for 512 of 128.
+//     2040 x 2048 x 2048: 14.0 with 128, 25.6 with 256; 32000 x 2048 x 2048: 152 with 128, 121 with 256.
 template <Num T>
 hipError_t product_typed(const ProductArgs &p, hipStream_t stream)
 {
-    if (p.M <= 64) return direct<T, false, 1, 1, 4, 4>(p, stream);
-    if (p.N <= 32) return direct<T, false, 2, 2, 4, 1>(p, stream);
-    if ((int64_t)((p.M + kTile - 1) / kTile) * ((p.N + kTile - 1) / kTile) >= 64) return tiled<T>(p, stream);
-    return direct<T, false, 4, 4, 4, 1>(p, stream);
+    const int64_t small = small_tiles(p.M, p.N);
+    if (small <= 512) return direct<T, false, 1, 1, 4, 4>(p, stream);
+    if (small <= (p.K <= 128 ? 4096 : 1536)) return direct<T, false, 2, 2, 4, 4>(p, stream);
+    const int64_t large = (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256);
+    const int64_t mid = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
+    const double cost_large = (double)((large + 255) / 256) * (14.5 + 0.0075 * p.K);
+    const double cost_mid = std::max(1.0, (double)mid / 512) * (8.5 + 0.0052 * p.K);
+    return cost_large < cost_mid ? tiled<T, 4>(p, stream) : tiled<T, 2>(p, stream);
 }
 
 ProductArgs arguments(int M, int N, int K, const void *a, const uint8_t *a_scales, int64_t a_stride,
@@ -501,9 +532,16 @@ ProductArgs arguments(int M, int N, int K, const void *a, const uint8_t *a_scale
     return p;
 }
 
-// One pass over the plain rows where they are read about once: few columns of C (each workgroup of rows
-// quantises its rows for all of them), or so few rows that quantising them again costs nothing.
-bool linear_fused(int M, int N) { return N <= 64 || M <= 16; }
+// The plain rows are taken to codes where they are multiplied as long as that is not done too often (every
+// workgroup of columns does it again) and the operands need not be shared through LDS; else once, into a
+// workspace.  Measured (us, float rows, fused against packed): 100 x 28 x 256 4.0 / 7, 100000 x 28 x 1024 86 /
+// 107, 8000 x 64 x 1024 11.6 / 13.9, 32000 x 64 x 1024 34 / 32, 2040 x 1024 x 64 7.6 / 8.9 (bfloat16), 8000 x
+// 256 x 256 11.9 / 11.3, 8000 x 128 x 1024 19.4 / 15.2, 100 x 4096 x 4096 26 / 16.5 (bfloat16).
+bool linear_fused(int M, int N, int K)
+{
+    const int64_t small = small_tiles(M, N);
+    return N <= 32 || small <= 512 || small * K <= (N <= 64 ? 8000000 : 2000000);
+}
 
 }  // namespace
 
@@ -522,7 +560,7 @@ hipError_t launch_mx4_product(Num out, int M, int N, int K, const uint8_t *a_cod
 
 size_t mx4_linear_workspace(int M, int N, int K)
 {
-    if (linear_fused(M, N)) return 0;
+    if (linear_fused(M, N, K)) return 0;
     return (size_t)M * (mx_code_pitch(Mx::E2M1, K) + mx_scale_pitch(K));
 }
 
@@ -531,10 +569,14 @@ namespace {
 template <Num T>
 hipError_t linear_typed(const ProductArgs &p, void *workspace, hipStream_t stream)
 {
-    if (linear_fused(p.M, p.N)) {
-        if (p.M <= 64) return direct<T, true, 1, 1, 4, 4>(p, stream);
-        if (p.N <= 32) return direct<T, true, 2, 2, 4, 1>(p, stream);
-        return direct<T, true, 2, 4, 4, 1>(p, stream);
+    if (linear_fused(p.M, p.N, p.K)) {
+        // as above: a workgroup per 16 x 16 tile while there are few, with eight wavefronts along a long k (1 x
+        // 4096 x 4096 bfloat16: 6.9 against 8.2); else 64 rows by all of 32 or 64 columns, or 16 rows with the
+        // wavefronts along k where it is long (8000 x 64 x 1024: 11.6 against 18.9; x 256: 6.0 against 7.2)
+        if (small_tiles(p.M, p.N) <= 512)
+            return p.K >= 2048 ? direct<T, true, 1, 1, 8, 8>(p, stream) : direct<T, true, 1, 1, 4, 4>(p, stream);
+        if (p.K >= 1024) return direct<T, true, 1, 4, 4, 4>(p, stream);
+        return p.N <= 32 ? direct<T, true, 1, 2, 4, 1>(p, stream) : direct<T, true, 1, 4, 4, 1>(p, stream);
     }
     uint8_t *codes = (uint8_t *)workspace, *scales = codes + (int64_t)p.M * p.pitch;
     const hipError_t e = launch_mx_pack(Mx::E2M1, T, p.M, p.K, p.a, p.a_stride, codes, scales, stream);

@@ -124,19 +124,19 @@ def test_products_refuse(L):
     assert product(a=P + 8) == product(bsc=P + 2) == product(bias=P + 2) == product(out=P + 2) == EALIGN
 
     need = ctypes.c_size_t()
-    assert L.mg_mx4_linear_workspace(300, 300, 100, ctypes.byref(need)) == OK and need.value >= 300 * (16 * 4 + 4)
+    assert L.mg_mx4_linear_workspace(3000, 3000, 1000, ctypes.byref(need)) == OK and need.value >= 3000 * (16 * 32 + 32)
     size = need.value
     assert L.mg_mx4_linear_workspace(300, 28, 100, ctypes.byref(need)) == OK and need.value == 0
     assert L.mg_mx4_linear_workspace(300, 0, 100, ctypes.byref(need)) == ESHAPE
     assert L.mg_mx4_linear_workspace(300, 300, 100, None) == ENULL
 
-    def linear(dtype=0, M=300, N=300, K=100, x=P, xs=100, w=P, wsc=P, bias=None, out=P, stride=300, ws=P, size=size):
+    def linear(dtype=0, M=3000, N=3000, K=1000, x=P, xs=1000, w=P, wsc=P, bias=None, out=P, stride=3000, ws=P, size=size):
         return L.mg_mx4_linear(dtype, M, N, K, x, xs, w, wsc, bias, out, stride, ws, size, None)
 
     for k in ("x", "w", "wsc", "out"):
         assert linear(**{k: None}) == ENULL
     assert linear(dtype=-1) == EPARAM
-    assert linear(M=0) == linear(xs=99) == linear(stride=299) == ESHAPE
+    assert linear(M=0) == linear(xs=999) == linear(stride=2999) == ESHAPE
     assert linear(x=P + 1) == linear(w=P + 8) == linear(wsc=P + 1) == linear(out=P + 3) == EALIGN
     assert linear(ws=None) == linear(ws=P + 8) == linear(size=size - 1) == EWORKSPACE
 
