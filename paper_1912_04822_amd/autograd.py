@@ -8,14 +8,23 @@ gradient will be asked for, forward builds the tables once (``mg_prepare``) in a
 own and both passes run on them (the ``*_prepared`` calls): the backward pass then starts without
 a prep kernel.
 A binary GridMaker has no gradient (the indicator is piecewise constant); asking for one raises.
+
+Two things beside it, on the microscaled formats of the binding (blocks of 32 numbers that share a
+power of two): ``AtomTyper`` learns types from atom features -- the weights a vector-typed grid takes
+are a linear map of them -- and keeps its input in 8 bits for the weight gradient, or runs in 4 bits
+where no gradient is wanted; ``saved_in_8_bits`` keeps what a whole network saves for its backward
+pass in 8 bits.
 """
 from __future__ import annotations
 
+import threading
 from typing import Optional
 
 import torch
 
 from . import molgrid
+
+_exact = threading.local()          # set while a layer of this module saves what has to stay exact
 
 
 class _IndexGrid(torch.autograd.Function):
@@ -76,10 +85,181 @@ class _VectorGrid(torch.autograd.Function):
         return (gc if want_c else None, gw if want_w else None) + (None,) * 6
 
 
+class _Exact:
+    """What is saved inside stays as it is, also within ``saved_in_8_bits``."""
+
+    def __enter__(self):
+        self.before = getattr(_exact, "on", False)
+        _exact.on = True
+
+    def __exit__(self, *_):
+        _exact.on = self.before
+
+
+class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
+    """Within ``with saved_in_8_bits():`` what autograd saves for the backward pass is kept in 8 bits
+    (blocks of 32 neighbouring numbers in memory that share a power of two) and restored when it is
+    needed: a quarter of the memory of float32 activations, half of 16-bit ones.  For the network
+    behind a grid, whose activations are as large as the grid:
+
+        with saved_in_8_bits():
+            loss = net(layer(coords, radii, types=types, T=T))
+        loss.backward()
+
+    Kept so: float32, float16 and bfloat16 device tensors of at least ``min_elements`` numbers that
+    lie without gaps in memory, but for parameters (leaves that require a gradient) and views of them,
+    which exist anyway.  Everything else, and what this module's own layers save, stays exact.  ``format``
+    "int8" is off by at most 2^-7 of the block's largest number, "e4m3" by at most 2^-4 of each.
+    Gradients change accordingly; small positive numbers of a block may become zero (and with them
+    the gradient of a ReLU there), and a block that holds an infinity or a NaN becomes NaN."""
+
+    def __init__(self, format="int8", min_elements=1 << 16):
+        if format not in ("int8", "e4m3"):
+            raise ValueError("format must be int8 or e4m3, got %r" % (format,))
+        if min_elements < 1:
+            raise ValueError("min_elements must be at least 1")
+        self.format, self.min_elements = format, int(min_elements)
+        super().__init__(self._pack, self._unpack)
+
+    def _pack(self, x):
+        if (getattr(_exact, "on", False) or not x.is_cuda or x.dtype not in molgrid.NUMBERS
+                or x.numel() < self.min_elements or x.layout is not torch.strided
+                or _is_parameter(x) or (x._base is not None and _is_parameter(x._base))):
+            return x
+        flat = _in_memory_order(x.detach())
+        if flat is None:
+            return x
+        return molgrid.mg_mx_pack(flat, self.format), x.shape, x.stride()
+
+    @staticmethod
+    def _unpack(kept):
+        if isinstance(kept, torch.Tensor):
+            return kept
+        packed, shape, stride = kept
+        flat = molgrid.mg_mx_unpack(packed)
+        return flat.as_strided(shape, stride)
+
+
+def _is_parameter(x):
+    return x.is_leaf and x.requires_grad
+
+
+def _in_memory_order(x):
+    """``x`` as one row [1, numel], or None where its memory has gaps or is used twice."""
+    if not x.is_contiguous():
+        x = x.permute(sorted(range(x.dim()), key=lambda d: (-x.stride(d), -x.shape[d])))
+        if not x.is_contiguous():
+            return None
+    return x.view(1, -1)
+
+
+class _TypeWeights(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, features, weight, bias, natoms, keep):
+        y = torch.nn.functional.linear(features, weight, bias)
+        packed = molgrid.mg_mx_pack(features, keep) if ctx.needs_input_grad[1] else None
+        ctx.keep = keep
+        ctx.shape, ctx.dtypes = features.shape, (features.dtype, weight.dtype, None if bias is None else bias.dtype)
+        ctx.save_for_backward(weight, natoms, *((packed.codes, packed.scales) if packed is not None else (None, None)))
+        return y.float()
+
+    @staticmethod
+    @torch.autograd.function.once_differentiable
+    def backward(ctx, grad):
+        weight, natoms, codes, scales = ctx.saved_tensors
+        gx = gw = gb = None
+        grad = grad.contiguous()
+        if natoms is not None and (ctx.needs_input_grad[0] or not ctx.needs_input_grad[1]):
+            grad = _live_rows(grad, natoms)
+        if ctx.needs_input_grad[0]:
+            gx = torch.matmul(grad.view(-1, grad.shape[2]), weight.float()).view(ctx.shape).to(ctx.dtypes[0])
+        if ctx.needs_input_grad[1]:
+            packed = molgrid.MXTensor(codes, scales, ctx.shape, ctx.keep)
+            gw, gb = molgrid.mg_mx8_weight_gradient(grad, packed, natoms=natoms)
+            gw = gw.to(ctx.dtypes[1])
+        if ctx.dtypes[2] is None or not ctx.needs_input_grad[2]:
+            gb = None
+        else:
+            if gb is None:                          # a bias alone
+                gb = grad.view(-1, grad.shape[2]).sum(0)
+            gb = gb.to(ctx.dtypes[2])
+        return gx, gw, gb, None, None
+
+
+def _live_rows(x, natoms):
+    """``x`` [B,N,...] with zeros past every example's ``natoms``."""
+    live = torch.arange(x.shape[1], device=x.device)[None, :] < natoms[:, None]
+    return torch.where(live[:, :, None], x, torch.zeros((), dtype=x.dtype, device=x.device))
+
+
+class AtomTyper(torch.nn.Module):
+    """Learned vector types: ``typer(features)`` maps per-atom features [B,N,E] (float32, float16 or
+    bfloat16) linearly to type weights [B,N,T] in float32, which a vector-typed grid takes
+    (``GridLayer(..., typer=AtomTyper(E, T))`` and ``layer(coords, radii, features=features)``).
+
+    What the weight gradient needs of the features is kept in 8 bits (``keep`` "int8" or "e4m3") and
+    the gradient formed from the codes; ``keep=None`` leaves both to torch.  With ``natoms`` [B] (int32)
+    atoms past an example's count have no part in any gradient, whatever their rows hold."""
+
+    def __init__(self, features, channels, bias=True, keep="int8", device=None, dtype=None):
+        super().__init__()
+        if keep not in (None, "int8", "e4m3"):
+            raise ValueError("keep must be int8, e4m3 or None, got %r" % (keep,))
+        if features < 1 or channels < 1:
+            raise ValueError("features and channels must be at least 1")
+        self.keep = keep
+        self.weight = torch.nn.Parameter(torch.empty((channels, features), device=device, dtype=dtype))
+        self.bias = torch.nn.Parameter(torch.empty((channels,), device=device, dtype=dtype)) if bias else None
+        bound = features ** -0.5
+        torch.nn.init.uniform_(self.weight, -bound, bound)
+        if bias:
+            torch.nn.init.uniform_(self.bias, -bound, bound)
+
+    def forward(self, features, natoms=None):
+        if features.dim() != 3 or features.shape[2] != self.weight.shape[1]:
+            raise ValueError("features must have shape [B,N,%d], got %s"
+                             % (self.weight.shape[1], tuple(features.shape)))
+        if self.keep is None or not torch.is_grad_enabled():
+            if natoms is not None and torch.is_grad_enabled():
+                features = _live_rows(features, natoms)
+            return torch.nn.functional.linear(features, self.weight, self.bias).float()
+        with _Exact():
+            return _TypeWeights.apply(features, self.weight, self.bias, natoms, self.keep)
+
+    def in_4_bits(self):
+        """A copy for use without gradients (screening), its weights laid out in 4 bits once."""
+        return AtomTyper4(self.weight, self.bias)
+
+
+class AtomTyper4(torch.nn.Module):
+    """``AtomTyper`` where no gradient is wanted: features and weights enter the product in 4 bits
+    (e2m1, a power of two for every 32 features), sums are float.  Made by ``AtomTyper.in_4_bits``
+    from the weights of that moment; ``state_dict`` holds the codes."""
+
+    def __init__(self, weight, bias=None):
+        super().__init__()
+        packed = molgrid.mg_mx_pack(weight.detach().contiguous(), "e2m1")
+        self.features = weight.shape[1]
+        self.register_buffer("codes", packed.codes)
+        self.register_buffer("scales", packed.scales)
+        self.register_buffer("bias", None if bias is None else bias.detach().float().clone())
+
+    def forward(self, features, natoms=None):
+        """``natoms`` is taken for the sake of ``AtomTyper``'s signature: every row is mapped."""
+        if torch.is_grad_enabled() and features.requires_grad:
+            raise RuntimeError("a typer in 4 bits has no gradient")
+        if features.dim() != 3 or features.shape[2] != self.features:
+            raise ValueError("features must have shape [B,N,%d], got %s" % (self.features, tuple(features.shape)))
+        weight = molgrid.MXTensor(self.codes, self.scales, (self.codes.shape[0], self.features), "e2m1")
+        bias = None if self.bias is None else self.bias.float()
+        return molgrid.mg_mx4_linear(features, weight, bias).float()
+
+
 class GridLayer(torch.nn.Module):
     """A GridMaker as a differentiable layer: ``layer(coords, types=... | weights=..., ...)``
     returns the ``[B,T,D,D,D]`` grid (``[B,S,S,S,T,D,D,D]`` with ``subgrids_per_side`` = S > 1);
-    gradients flow to ``coords`` (and ``weights``).
+    gradients flow to ``coords`` (and ``weights``).  With a ``typer`` (``AtomTyper`` or
+    ``AtomTyper4``) it also takes ``features`` [B,N,E], whose type weights the typer computes.
 
     ``random_rotation`` / ``random_translation`` (GridMaker.forward's optional augmentation): a
     fresh per-example rotation and a translation of at most that many Angstrom per axis are
@@ -88,8 +268,9 @@ class GridLayer(torch.nn.Module):
     applied transformation can be retained; gradients come back in the caller's frame."""
 
     def __init__(self, resolution=0.5, dimension=23.5, binary=False, radius_type_indexed=True,
-                 radius_scale=1.0, gaussian_radius_multiple=1.0, subgrids_per_side=1):
+                 radius_scale=1.0, gaussian_radius_multiple=1.0, subgrids_per_side=1, typer=None):
         super().__init__()
+        self.typer = typer
         self.gm = molgrid.GridMaker(resolution, dimension, binary=binary,
                                     radius_type_indexed=radius_type_indexed,
                                     radius_scale=radius_scale,
@@ -101,7 +282,13 @@ class GridLayer(torch.nn.Module):
     def forward(self, coords, radii, *, types: Optional[torch.Tensor] = None,
                 weights: Optional[torch.Tensor] = None, T: Optional[int] = None, natoms=None,
                 centers=None, quats=None, translations=None, random_rotation=False,
-                random_translation=0.0):
+                random_translation=0.0, features: Optional[torch.Tensor] = None):
+        if features is not None:
+            if self.typer is None:
+                raise ValueError("features need a typer (GridLayer(..., typer=AtomTyper(E, T)))")
+            if types is not None or weights is not None:
+                raise ValueError("give features, types or weights, not two of them")
+            weights = self.typer(features, natoms)
         if (types is None) == (weights is None):
             raise ValueError("give exactly one of types (index) or weights (vector)")
         if random_rotation or random_translation > 0.0:
@@ -115,7 +302,9 @@ class GridLayer(torch.nn.Module):
         if types is not None:
             if T is None:
                 raise ValueError("index types need the number of channels T")
-            return _IndexGrid.apply(coords, self.gm, types, radii, T, natoms, centers, quats,
-                                    translations)
-        return _VectorGrid.apply(coords, weights, self.gm, radii, natoms, centers, quats,
-                                 translations)
+            with _Exact():
+                return _IndexGrid.apply(coords, self.gm, types, radii, T, natoms, centers, quats,
+                                        translations)
+        with _Exact():
+            return _VectorGrid.apply(coords, weights, self.gm, radii, natoms, centers, quats,
+                                     translations)

@@ -455,7 +455,7 @@ class GridMaker:
 # ---- microscaled formats: numbers in 8 or 4 bits ----
 
 MX_FORMATS = {"int8": 0, "e4m3": 1, "e2m1": 2}          # MG_MX_INT8, MG_MX_E4M3, MG_MX_E2M1
-_NUMBERS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # MG_F32, MG_F16, MG_BF16
+NUMBERS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # MG_F32, MG_F16, MG_BF16
 
 
 class MXTensor:
@@ -540,7 +540,7 @@ def _optional(t, dtype, name, shape, dev):
 
 
 def _number(dtype, name):
-    code = _NUMBERS.get(dtype)
+    code = NUMBERS.get(dtype)
     if code is None:
         raise TypeError("%s must be float32, float16 or bfloat16, got %s" % (name, dtype))
     return code

@@ -1,0 +1,329 @@
+"""Layers on microscaled formats: learned types (AtomTyper, AtomTyper4) alone and in front of a grid,
+and networks whose saved tensors are kept in 8 bits.  What is kept is known to the bit (the reference's
+codes), so gradients are compared with their formulas at the kept values; and with differences of the
+loss, within the error that 8 bits can make."""
+import numpy as np
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_1912_04822_amd import molgrid, workloads  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, AtomTyper4, GridLayer, saved_in_8_bits  # noqa: E402
+from mx_reference import product_bound, values  # noqa: E402
+
+
+def dev(a):
+    return torch.from_numpy(np.ascontiguousarray(a)).cuda()
+
+
+def kept(x, fmt):
+    """[B,N,E] -> what the 8-bit codes of its rows stand for, float64 on the host."""
+    a = x.detach().double().cpu().numpy()
+    return torch.from_numpy(values(a.reshape(-1, a.shape[-1]), fmt).reshape(a.shape))
+
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("ragged", [False, True])
+def test_typer_gradients(fmt, dtype, ragged):
+    torch.manual_seed(1)
+    B, N, E, T = 3, 70, 45, 6
+    typer = AtomTyper(E, T, keep=fmt).cuda().to(dtype)
+    x = torch.randn((B, N, E), device="cuda").to(dtype)
+    live = torch.ones((B, N), dtype=torch.bool)
+    natoms = None
+    if ragged:
+        n = torch.tensor([70, 0, 13], dtype=torch.int32)
+        live = torch.arange(N)[None] < n[:, None]
+        natoms = n.cuda()
+        x[~live.cuda()] = float("nan")
+    x.requires_grad_()
+    y = typer(x, natoms)
+    assert y.dtype == torch.float32 and y.shape == (B, N, T)
+    want_y = torch.nn.functional.linear(x.detach(), typer.weight.detach(), typer.bias.detach()).float()
+    assert torch.equal(y[live.cuda()], want_y[live.cuda()])
+    G = torch.randn((B, N, T), device="cuda")
+    y.backward(G)
+    g, xk = G.double().cpu()[live], kept(x, fmt)[live]
+    half = torch.finfo(dtype).eps / 2
+    bound = lambda s, v: 3 * len(g) * 2.0 ** -24 * s + half * v.abs() + 1e-30
+    want_w, want_b = g.t() @ xk, g.sum(0)
+    assert ((typer.weight.grad.double().cpu() - want_w).abs() <= bound(g.abs().t() @ xk.abs(), want_w) * 1.01).all()
+    assert ((typer.bias.grad.double().cpu() - want_b).abs() <= bound(g.abs().sum(0), want_b) * 1.01).all()
+    w = typer.weight.detach().double().cpu()
+    want_x = torch.where(live[:, :, None], G.double().cpu(), torch.zeros((), dtype=torch.float64)) @ w
+    tol = T * 2.0 ** -23 * (G.double().cpu().abs() @ w.abs()) + half * want_x.abs() + 1e-7
+    assert ((x.grad.double().cpu() - want_x).abs() <= tol).all()
+    if ragged:
+        assert (x.grad[~live.cuda()] == 0).all()
+
+
+def test_typer_gradient_against_differences():
+    """The loss is linear in the weights: a difference of it is the exact gradient, which the kept one
+    misses by at most half a step of every number (2^-7 of its block's largest)."""
+    torch.manual_seed(2)
+    B, N, E, T = 2, 200, 64, 5
+    typer = AtomTyper(E, T, bias=False).cuda()
+    x = torch.randn((B, N, E), device="cuda")
+    G = torch.randn((B, N, T), device="cuda")
+    (typer(x) * G).sum().backward()
+    w = typer.weight.detach().double()
+    loss = lambda v: float((torch.matmul(x.double(), v.t()) * G.double()).sum())
+    big = x.abs().view(B, N, E // 32, 32).amax(3).repeat_interleave(32, 2).double()
+    off = torch.einsum("bnt,bne->te", G.abs().double().cpu(), big.cpu() * 2.0 ** -6)
+    rng = np.random.default_rng(0)
+    for _ in range(8):
+        t, e = int(rng.integers(T)), int(rng.integers(E))
+        h = torch.zeros_like(w)
+        h[t, e] = 0.5
+        diff = loss(w + h) - loss(w - h)
+        assert abs(float(typer.weight.grad[t, e]) - diff) <= float(off[t, e]) + 1e-3 * abs(diff) + 1e-3
+
+
+def test_only_what_is_asked_for():
+    x = torch.randn((1, 40, 33), device="cuda")
+    typer = AtomTyper(33, 4).cuda()
+    typer.weight.requires_grad_(False)
+    (typer(x, torch.tensor([30], dtype=torch.int32, device="cuda")) * 2).sum().backward()
+    assert typer.weight.grad is None and torch.allclose(typer.bias.grad, torch.full((4,), 60.0, device="cuda"))
+    typer = AtomTyper(33, 4, bias=False).cuda()
+    typer(x).sum().backward()
+    assert typer.weight.grad.shape == (4, 33)
+    with torch.no_grad():
+        assert not typer(x).requires_grad
+
+
+def test_typer_in_4_bits():
+    torch.manual_seed(3)
+    typer = AtomTyper(90, 28).cuda()
+    four = typer.in_4_bits()
+    x = torch.randn((3, 50, 90), device="cuda")
+    y = four(x)
+    a, w = values(x.double().cpu().numpy().reshape(-1, 90), "e2m1"), values(typer.weight.detach().double().cpu().numpy(), "e2m1")
+    b = typer.bias.detach().double().cpu().numpy()
+    want = a @ w.T + b
+    err = np.abs(y.double().cpu().numpy().reshape(-1, 28) - want)
+    assert (err <= product_bound(a, w) + 2.0 ** -22 * (np.abs(want) + np.abs(b))).all()
+    with pytest.raises(RuntimeError):
+        four(x.clone().requires_grad_())
+    with pytest.raises(ValueError):
+        four(x[:, :, :80])
+    again = AtomTyper4(torch.zeros((28, 90), device="cuda"), torch.zeros((28,), device="cuda"))
+    again.load_state_dict(four.state_dict())
+    assert torch.equal(again(x), y)
+    typer.weight.data.mul_(2.0)                      # a copy of that moment
+    assert torch.equal(four(x), y)
+
+
+def grid_case(B=2, seed=5):
+    w = workloads.ragged_small(seed=seed, B=B, N=120, T=5, D=12, resolution=0.5)
+    return w, dict(centers=dev(w.centers), quats=dev(w.quats), translations=dev(w.translations))
+
+
+def test_grid_layer_with_a_typer_is_the_typer_and_the_grid():
+    w, pose = grid_case()
+    torch.manual_seed(4)
+    layer = GridLayer(w.resolution, w.dimension, typer=AtomTyper(40, w.T).cuda())
+    n = torch.tensor([w.N, w.N // 2], dtype=torch.int32, device="cuda")
+    x = torch.randn((w.B, w.N, 40), device="cuda")
+    x[1, w.N // 2:] = float("nan")
+    G = torch.randn(w.out_shape, device="cuda")
+
+    def leaves():
+        return dev(w.coords).requires_grad_(), x.clone().requires_grad_()
+
+    c1, x1 = leaves()
+    grid = layer(c1, dev(w.radii), features=x1, natoms=n, **pose)
+    got = torch.autograd.grad((grid * G).sum(), [c1, x1] + list(layer.parameters()))
+    c2, x2 = leaves()
+    weights = layer.typer(x2, n)
+    want_grid = GridLayer(w.resolution, w.dimension)(c2, dev(w.radii), weights=weights, natoms=n, **pose)
+    want = torch.autograd.grad((want_grid * G).sum(), [c2, x2] + list(layer.parameters()))
+    assert torch.equal(grid, want_grid) and torch.isfinite(grid).all()
+    for a, b in zip(got, want):
+        assert torch.equal(a, b) and torch.isfinite(a).all()
+    assert got[2].abs().max() > 0 and (got[1][1, w.N // 2:] == 0).all()
+
+
+# ---- tensors a network saves ----
+
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("dtype", [torch.float32, torch.float16, torch.bfloat16], ids=str)
+def test_saved_tensors_are_their_codes(fmt, dtype):
+    x = torch.randn((3, 4, 7, 9, 11), device="cuda").to(dtype).requires_grad_()
+    h = x * 1.0                                     # not a leaf: an activation
+    h.retain_grad()
+    with saved_in_8_bits(fmt, min_elements=1000):
+        y = h.square()
+    y.backward(torch.ones_like(y))
+    k = values(h.detach().double().cpu().numpy().reshape(1, -1), fmt).reshape(h.shape)
+    assert torch.equal(h.grad.double().cpu(), torch.from_numpy(k).mul(2).to(dtype).double())
+
+
+def test_layouts_small_tensors_and_parameters():
+    seen = []
+
+    class Look(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, *xs):
+            ctx.save_for_backward(*xs)
+            return xs[0] * 1.0
+
+        @staticmethod
+        def backward(ctx, g):
+            seen.extend(ctx.saved_tensors)
+            return (g,) + (None,) * (len(ctx.saved_tensors) - 1)
+
+    last = torch.randn((2, 8, 5, 6, 7), device="cuda").to(memory_format=torch.channels_last_3d).requires_grad_() * 1.0
+    swapped = torch.randn((40, 50), device="cuda").t()
+    gaps = torch.randn((40, 100), device="cuda")[:, ::2]
+    wide = torch.randn((40, 1), device="cuda").expand(40, 50)
+    small = torch.randn((999,), device="cuda")
+    whole = torch.arange(2000, device="cuda")
+    double = torch.randn((2000,), device="cuda", dtype=torch.float64)
+    par = torch.nn.Parameter(torch.randn((50, 40), device="cuda"))
+    xs = [last, swapped, gaps, wide, small, whole, double, par, par.t()]
+    with saved_in_8_bits(min_elements=1000):
+        Look.apply(*xs).sum().backward()
+    assert len(seen) == len(xs)
+    for i, (a, b) in enumerate(zip(seen, xs)):
+        assert a.shape == b.shape and a.stride() == b.stride() and a.dtype == b.dtype
+        assert torch.equal(a, b) == (i >= 2), i
+    order = last.detach().permute(0, 2, 3, 4, 1).reshape(1, -1).double().cpu().numpy()
+    want = torch.from_numpy(values(order, "int8")).view(2, 5, 6, 7, 8).permute(0, 4, 1, 2, 3)
+    assert torch.equal(seen[0].double().cpu(), want)
+
+
+def test_memory_goes_down_and_a_network_still_learns_its_gradients():
+    """A small network of ReLU layers over a large activation: the saved tensors take a bit more than a
+    quarter, and every gradient lies within what 2^-7 of a block's largest number can change."""
+    torch.manual_seed(6)
+    n = 1 << 20
+    x = torch.randn((4, n), device="cuda")
+    ws = [torch.randn((4, 1), device="cuda").requires_grad_() for _ in range(3)]
+
+    def loss():
+        h = x
+        for w in ws:
+            h = torch.nn.functional.softplus(h * w)
+        return h.mean()
+
+    torch.cuda.synchronize()
+    base = torch.cuda.memory_allocated()
+    plain = loss()
+    torch.cuda.synchronize()
+    full = torch.cuda.memory_allocated() - base
+    want = torch.autograd.grad(plain, ws)
+    del plain
+    with saved_in_8_bits():
+        kept8 = loss()
+    torch.cuda.synchronize()
+    less = torch.cuda.memory_allocated() - base
+    got = torch.autograd.grad(kept8, ws)
+    assert less < 0.45 * full
+    for a, b in zip(got, want):
+        assert (a - b).abs().max() <= 0.02 * b.abs().max() + 1e-3
+
+
+def test_grid_layers_save_exactly_within_the_context():
+    w, pose = grid_case(B=3, seed=7)
+    rng = np.random.default_rng(8)
+    wts = dev(rng.dirichlet(0.3 * np.ones(w.T), (w.B, w.N)).astype(np.float32))
+    layer = GridLayer(w.resolution, w.dimension)
+    G = torch.randn(w.out_shape, device="cuda")
+
+    def grads(inside):
+        c, v = dev(w.coords).requires_grad_(), (wts * 1.0).requires_grad_()
+        if inside:
+            with saved_in_8_bits(min_elements=1):
+                grid = layer(c, dev(w.radii), weights=v * 1.0, **pose)
+        else:
+            grid = layer(c, dev(w.radii), weights=v * 1.0, **pose)
+        return torch.autograd.grad((grid * G).sum(), [c, v])
+
+    for a, b in zip(grads(True), grads(False)):
+        assert torch.equal(a, b)
+
+
+def test_all_together_as_a_training_step_and_a_screening():
+    """Features to types (8 bits kept), grid, a network whose tensors are saved in 8 bits, gradients to
+    everything; two optimiser steps; then screening in 4 bits.  Against the same step without any of it:
+    within the errors 8 bits make."""
+    w, pose = grid_case(B=4, seed=9)
+    torch.manual_seed(10)
+    E = 48
+    x = torch.randn((w.B, w.N, E), device="cuda")
+    n = torch.tensor([w.N, 60, 1, 0], dtype=torch.int32, device="cuda")
+    mix = torch.nn.Parameter(0.3 * torch.randn((16, w.T), device="cuda"))
+    out = torch.nn.Parameter(torch.randn((16,), device="cuda"))
+
+    def step(layer, context):
+        c = dev(w.coords).requires_grad_()
+        with context:
+            grid = layer(c, dev(w.radii), features=x, natoms=n, **pose)
+            h = torch.tanh(torch.matmul(mix, grid.reshape(w.B, w.T, -1)))
+            loss = (h * out[None, :, None]).square().mean()
+        params = [c, mix, out] + list(layer.parameters())
+        return loss.detach(), torch.autograd.grad(loss, params)
+
+    import contextlib
+    typer = AtomTyper(E, w.T).cuda()
+    plain = AtomTyper(E, w.T, keep=None).cuda()
+    plain.load_state_dict(typer.state_dict())
+    layer, other = GridLayer(w.resolution, w.dimension, typer=typer), GridLayer(w.resolution, w.dimension, typer=plain)
+    for _ in range(2):
+        loss, grads = step(layer, saved_in_8_bits(min_elements=1))
+        want_loss, want = step(other, contextlib.nullcontext())
+        assert torch.allclose(loss, want_loss, rtol=1e-5)
+        for a, b in zip(grads, want):
+            assert torch.isfinite(a).all()
+            assert (a - b).norm() <= 0.05 * b.norm()
+        with torch.no_grad():
+            for p, q, g in zip(layer.parameters(), other.parameters(), want[3:]):
+                p -= 0.1 * g
+                q -= 0.1 * g
+    with torch.no_grad():
+        screen = GridLayer(w.resolution, w.dimension, typer=typer.in_4_bits())
+        got = screen(dev(w.coords), dev(w.radii), features=x, natoms=n, **pose)
+        weights = typer.in_4_bits()(x)
+        assert torch.equal(got, GridLayer(w.resolution, w.dimension)(dev(w.coords), dev(w.radii), weights=weights,
+                                                                    natoms=n, **pose))
+        full = layer(dev(w.coords), dev(w.radii), features=x, natoms=n, **pose)
+        assert (got - full).norm() <= 0.3 * full.norm()
+
+
+def test_screening_in_a_graph():
+    w, pose = grid_case(B=2, seed=11)
+    typer = AtomTyper(64, w.T).cuda().in_4_bits()
+    layer = GridLayer(w.resolution, w.dimension, typer=typer)
+    x = torch.randn((w.B, w.N, 64), device="cuda")
+    coords, radii = dev(w.coords), dev(w.radii)
+    with torch.no_grad():
+        layer(coords, radii, features=x, **pose)
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            out = layer(coords, radii, features=x, **pose)
+        for k in range(4):
+            x.normal_()
+            graph.replay()
+            torch.cuda.synchronize()
+            assert torch.equal(out, layer(coords, radii, features=x, **pose)), k
+
+
+def test_tensors_on_another_stream():
+    x = torch.randn((2, 500, 100), device="cuda")
+    typer = AtomTyper(100, 8).cuda()
+    G = torch.randn((2, 500, 8), device="cuda")
+    typer(x).backward(G)
+    want = typer.weight.grad.clone()
+    torch.cuda.synchronize()
+    s = torch.cuda.Stream()
+    typer.weight.grad = None
+    with torch.cuda.stream(s):
+        typer(x).backward(G)
+    s.synchronize()
+    torch.cuda.synchronize()
+    assert torch.equal(typer.weight.grad, want)
+    assert molgrid.mg_mx_pack(x).codes.device == x.device
