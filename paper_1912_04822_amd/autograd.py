@@ -157,7 +157,7 @@ class _TypeWeights(torch.autograd.Function):
     @staticmethod
     def forward(ctx, features, weight, bias, natoms, keep):
         y = torch.nn.functional.linear(features, weight, bias)
-        packed = molgrid.mg_mx_pack(features, keep) if ctx.needs_input_grad[1] else None
+        packed = molgrid.mg_mx_pack(_even_rows(features), keep) if ctx.needs_input_grad[1] else None
         ctx.keep = keep
         ctx.shape, ctx.dtypes = features.shape, (features.dtype, weight.dtype, None if bias is None else bias.dtype)
         ctx.save_for_backward(weight, natoms, *((packed.codes, packed.scales) if packed is not None else (None, None)))
@@ -184,6 +184,17 @@ class _TypeWeights(torch.autograd.Function):
                 gb = grad.view(-1, grad.shape[2]).sum(0)
             gb = gb.to(ctx.dtypes[2])
         return gx, gw, gb, None, None
+
+
+def _even_rows(x):
+    """``x``, or a copy where its rows are not equally far apart (expanded, transposed)."""
+    return x if molgrid.row_stride(x) is not None else x.contiguous()
+
+
+def _check_natoms(natoms, features):
+    if natoms is not None and (natoms.dtype is not torch.int32 or tuple(natoms.shape) != (features.shape[0],)):
+        raise ValueError("natoms must be int32 of shape (%d,), got %s of %s"
+                         % (features.shape[0], natoms.dtype, tuple(natoms.shape)))
 
 
 def _live_rows(x, natoms):
@@ -219,6 +230,7 @@ class AtomTyper(torch.nn.Module):
         if features.dim() != 3 or features.shape[2] != self.weight.shape[1]:
             raise ValueError("features must have shape [B,N,%d], got %s"
                              % (self.weight.shape[1], tuple(features.shape)))
+        _check_natoms(natoms, features)
         if self.keep is None or not torch.is_grad_enabled():
             if natoms is not None and torch.is_grad_enabled():
                 features = _live_rows(features, natoms)
@@ -252,7 +264,7 @@ class AtomTyper4(torch.nn.Module):
             raise ValueError("features must have shape [B,N,%d], got %s" % (self.features, tuple(features.shape)))
         weight = molgrid.MXTensor(self.codes, self.scales, (self.codes.shape[0], self.features), "e2m1")
         bias = None if self.bias is None else self.bias.float()
-        return molgrid.mg_mx4_linear(features, weight, bias).float()
+        return molgrid.mg_mx4_linear(_even_rows(features), weight, bias).float()
 
 
 class GridLayer(torch.nn.Module):

@@ -16,6 +16,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmolgrid_hip.so")
 
 MG_OK = 0
+MG_EWORKSPACE = -4
 EXPORTS = [
     "mg_gridmaker_create", "mg_gridmaker_create_subgrids", "mg_gridmaker_subgrids_per_side",
     "mg_gridmaker_destroy", "mg_gridmaker_points_per_side",
@@ -510,7 +511,10 @@ def _mx_pointers(t, name, formats, dev):
     codes, scales = t.codes, t.scales
     if codes.get_device() != dev or scales.get_device() != dev:
         _refuse_device(dev, **{name + ".codes": codes, name + ".scales": scales})
-    return (rows, cols, _ptr(codes, torch.uint8, name + ".codes", cshape),
+    if (dev >= 0 and codes.dtype is scales.dtype is torch.uint8 and codes.shape == cshape and scales.shape == sshape
+            and codes.is_contiguous() and scales.is_contiguous()):
+        return rows, cols, codes.data_ptr(), scales.data_ptr()
+    return (rows, cols, _ptr(codes, torch.uint8, name + ".codes", cshape),      # says what is wrong
             _ptr(scales, torch.uint8, name + ".scales", sshape))
 
 
@@ -546,12 +550,14 @@ def _number(dtype, name):
     return code
 
 
-def _row_stride(t, name):
-    """Elements from row to row of a tensor whose rows (last dimension) are equally far apart."""
+def row_stride(t):
+    """Elements from row to row of a tensor (a row: its last dimension), or None where rows are not
+    contiguous, not equally far apart, or overlap."""
     if t.is_contiguous():
-        return t.shape[-1]
-    if t.shape[-1] > 1 and t.stride(-1) != 1:
-        raise ValueError("the last dimension of %s must be contiguous" % name)
+        return t.size(-1)
+    cols = t.size(-1)
+    if cols > 1 and t.stride(-1) != 1:
+        return None
     step = unit = None
     for d in range(t.dim() - 2, -1, -1):        # the innermost dimension that has a step fixes it
         if t.shape[d] == 1:
@@ -559,12 +565,17 @@ def _row_stride(t, name):
         if step is None:
             step = unit = t.stride(d)
         elif t.stride(d) != unit:
-            raise ValueError("the rows of %s must be equally far apart" % name)
+            return None
         unit *= t.shape[d]
     if step is None:
-        return t.shape[-1]
-    if step < t.shape[-1]:
-        raise ValueError("the rows of %s overlap" % name)
+        return cols
+    return step if step >= cols else None
+
+
+def _row_stride(t, name):
+    step = row_stride(t)
+    if step is None:
+        raise ValueError("the rows of %s must be contiguous and equally far apart" % name)
     return step
 
 
@@ -574,8 +585,8 @@ _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.curre
 
 def _launch(fn, dev, *args):
     """One library call on the current stream of the tensors' device, whichever device is current."""
-    if dev == _current_device():
-        rc = fn(*args, _raw_stream(dev) if _raw_stream is not None else _stream())
+    if dev == _current_device() and _raw_stream is not None:
+        rc = fn(*args, _raw_stream(dev))
     else:
         with torch.cuda.device(dev):
             rc = fn(*args, _stream())
@@ -658,8 +669,8 @@ def _product_out(out, shape, dtype, like, dev):
     """The result's tensor and the stride of its rows."""
     if out is None:
         return like.new_empty(shape, dtype=dtype), shape[-1]
-    if tuple(out.shape) != shape:
-        raise ValueError("out must have shape %s, got %s" % (shape, tuple(out.shape)))
+    if tuple(out.shape) != tuple(shape):
+        raise ValueError("out must have shape %s, got %s" % (tuple(shape), tuple(out.shape)))
     if out.dtype != dtype:
         raise TypeError("out must be %s, got %s" % (dtype, out.dtype))
     if out.get_device() != dev:
@@ -691,13 +702,16 @@ def mg_mx4_linear(x, weight: MXTensor, bias=None, out=None):
     if shape[-1] != K:
         raise ValueError("rows of x have %d numbers, rows of weight %d" % (shape[-1], K))
     number, stride = _number(x.dtype, "x"), _row_stride(x, "x")
-    M = 1
-    for d in shape[:-1]:
-        M *= d
-    out, ostride = _product_out(out, tuple(shape[:-1]) + (N,), x.dtype, x, dev)
-    L = lib()
-    ws, size = _workspace_of(L.mg_mx4_linear_workspace, x, M, N, K)
-    _launch(L.mg_mx4_linear, dev, number, M, N, K, x.data_ptr(), stride, wc, wsc,
-            _optional(bias, torch.float32, "bias", (N,), dev), out.data_ptr(), ostride,
-            None if ws is None else ws.data_ptr(), size)
+    M = shape[0] if len(shape) == 2 else shape[:-1].numel()
+    out, ostride = _product_out(out, shape[:-1] + (N,), x.dtype, x, dev)
+    fn = lib().mg_mx4_linear
+    args = (number, M, N, K, x.data_ptr(), stride, wc, wsc, _optional(bias, torch.float32, "bias", (N,), dev),
+            out.data_ptr(), ostride)
+    try:                                        # most calls need no workspace: ask only where one does
+        _launch(fn, dev, *args, None, 0)
+    except MolgridError as e:
+        if e.code != MG_EWORKSPACE:
+            raise
+        ws, size = _workspace_of(lib().mg_mx4_linear_workspace, x, M, N, K)
+        _launch(fn, dev, *args, ws.data_ptr(), size)
     return out

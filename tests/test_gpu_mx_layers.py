@@ -327,3 +327,25 @@ def test_tensors_on_another_stream():
     torch.cuda.synchronize()
     assert torch.equal(typer.weight.grad, want)
     assert molgrid.mg_mx_pack(x).codes.device == x.device
+
+
+def test_features_of_any_layout():
+    """Expanded over the batch, transposed, a slice of wider rows: the gradients of a copy of them."""
+    torch.manual_seed(12)
+    typer = AtomTyper(33, 6).cuda()
+    G = torch.randn((4, 50, 6), device="cuda")
+    base = [torch.randn((1, 50, 33), device="cuda"), torch.randn((33, 50, 4), device="cuda"),
+            torch.randn((4, 50, 40), device="cuda"), torch.randn((50, 4, 33), device="cuda")]
+    views = [lambda b: b.expand(4, 50, 33), lambda b: b.permute(2, 1, 0), lambda b: b[:, :, 5:38],
+             lambda b: b.transpose(0, 1)]
+    for b, view in zip(base, views):
+        b.requires_grad_()
+        got = torch.autograd.grad(typer(view(b)), [b, typer.weight], G)
+        copy = view(b).detach().contiguous().requires_grad_()
+        want = torch.autograd.grad(typer(copy), [copy, typer.weight], G)
+        assert torch.equal(got[1], want[1])
+        back, = torch.autograd.grad(view(b), b, want[0])
+        assert torch.equal(got[0], back)
+        with torch.no_grad():
+            four = typer.in_4_bits()
+            assert torch.equal(four(view(b)), four(copy))

@@ -59,3 +59,22 @@ def test_host_tensors_are_saved_as_they_are():
         y = (x * x).sum()
     y.backward()
     assert torch.equal(x.grad, 2 * x.detach())
+
+
+def test_natoms_are_checked():
+    for keep in (None, "int8"):
+        typer = AtomTyper(8, 4, keep=keep)
+        for bad in (torch.tensor([1, 2]), torch.ones(3, dtype=torch.int32), torch.ones((2, 1), dtype=torch.int32)):
+            with pytest.raises(ValueError):
+                typer(torch.zeros((2, 3, 8)), bad)
+
+
+def test_rows_of_a_tensor():
+    from paper_1912_04822_amd.molgrid import row_stride
+    x = torch.zeros((4, 6, 10))
+    assert row_stride(x) == 10 and row_stride(x[:, :, 2:5]) == 10 and row_stride(x[:, :, :1]) == 10
+    assert row_stride(x[:, 1:3]) is None and row_stride(x[1:2, 1:3]) == 10 and row_stride(x[:, 1]) == 60
+    assert row_stride(x.transpose(0, 1)) is None and row_stride(x[:, :, ::2]) is None
+    assert row_stride(x[:1, :1].expand(4, 6, 10)) is None and row_stride(x[:1].expand(4, 6, 10)) is None
+    assert row_stride(torch.zeros(7)) == 7 and row_stride(torch.zeros((5, 1))) == 1
+    assert row_stride(torch.zeros(20).as_strided((3, 8), (4, 1))) is None
