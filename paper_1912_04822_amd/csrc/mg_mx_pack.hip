@@ -5,7 +5,9 @@
 // the plain numbers and the codes are moved in runs that are contiguous over the wavefront.  Magnitudes
 // are compared as unsigned words, where a NaN is larger than everything: a block that is not finite is
 // found by its maximum alone.  Both directions are bound by memory: a number is read or written once and
-// meets about a dozen instructions.
+// meets about a dozen instructions.  Measured, with a copy at 5.1 TB/s (read and written): 155 million floats
+// to int8 in 119 us and back in 110 (6.6 and 7.1 TB/s of their 0.78 GB), 22 million bfloat16 to e4m3 and back
+// in 13 each (5.1), 128000 odd rows of 509 halves to e2m1 in 37 (4.5) and back in 28.
 #include "mg_common.h"
 #include "mg_mx.h"
 
@@ -25,6 +27,17 @@ __device__ inline v4u load16(const void *p)
     return v;
 }
 __device__ inline void store16(void *p, v4u v) { __builtin_memcpy(p, &v, 16); }
+
+// A tensor that is larger than the memory-side cache is not found there by whoever comes next: it is read or
+// written past the caches (137 -> 119 and 131 -> 110 us for 0.62 GB of floats), aligned as it must be for that.
+// Smaller ones are not: what was just produced is still there, and what is restored is read again at once.
+constexpr int64_t kMemoryCacheBytes = 256ll << 20;
+
+bool streamed(const void *p, int64_t rows, int64_t row_stride, int64_t cols, int bytes)
+{
+    return rows * cols * bytes > kMemoryCacheBytes && ((uintptr_t)p & 15) == 0 &&
+           (rows == 1 || row_stride * bytes % 16 == 0);
+}
 
 template <Num T> constexpr int kPerLane = 16 / NumTraits<T>::bytes;
 
@@ -73,7 +86,7 @@ template <int Lanes> __device__ inline uint32_t block_max(uint32_t v)
 
 // Blocks are counted along the scale rows, whose length is a multiple of four: those past a row's last
 // block only clear their shared byte.
-template <Num T, Mx F, int Unroll>
+template <Num T, Mx F, int Unroll, bool Stream>
 __global__ __launch_bounds__(kThreads) void pack_kernel(const unsigned char *x, int64_t row_stride,
                                                         int64_t cols, uint32_t blocks, uint32_t pitch,
                                                         uint32_t total, uint8_t *codes, uint8_t *scales)
@@ -96,7 +109,8 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const unsigned char *x, 
             const int64_t c = (int64_t)blk[u] * kMxBlock + sub * P;
             const unsigned char *p = x + ((int64_t)row[u] * row_stride + c) * NumTraits<T>::bytes;
             if (c + P <= cols) {
-                raw[u] = load16(p);
+                if constexpr (Stream) raw[u] = __builtin_nontemporal_load((const v4u *)p);
+                else raw[u] = load16(p);
             } else if (c < cols) {                          // the end of a row
                 using E = typename NumTraits<T>::type;
                 E e[P];
@@ -153,7 +167,7 @@ template <Mx F> __device__ inline void decode4(uint32_t w, float *f)
     }
 }
 
-template <Num T, Mx F, int Unroll>
+template <Num T, Mx F, int Unroll, bool Stream>
 __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t *codes, const uint8_t *scales,
                                                           int64_t cols, uint32_t blocks, uint32_t pitch,
                                                           uint32_t total, unsigned char *x,
@@ -213,7 +227,8 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t *codes, 
         const int64_t c = (int64_t)blk[u] * kMxBlock + sub * P;
         unsigned char *p = x + ((int64_t)row[u] * row_stride + c) * NumTraits<T>::bytes;
         if (c + P <= cols) {
-            store16(p, out);
+            if constexpr (Stream) __builtin_nontemporal_store(out, (v4u *)p);
+            else store16(p, out);
         } else if (c < cols) {
             using E = typename NumTraits<T>::type;
             E e[P];
@@ -234,8 +249,10 @@ hipError_t pack_typed(int64_t rows, int64_t cols, const void *x, int64_t row_str
     const uint32_t blocks = (uint32_t)mx_blocks(cols), pitch = (uint32_t)mx_scale_pitch(cols);
     const uint32_t total = (uint32_t)(rows * pitch);
     constexpr uint32_t per = kThreads / (kMxBlock / kPerLane<T>) * kUnroll;
-    hipLaunchKernelGGL((pack_kernel<T, F, kUnroll>), dim3((total + per - 1) / per), dim3(kThreads), 0, stream,
-                       (const unsigned char *)x, row_stride, cols, blocks, pitch, total, codes, scales);
+    const auto kernel = streamed(x, rows, row_stride, cols, NumTraits<T>::bytes) ? pack_kernel<T, F, kUnroll, true>
+                                                                                : pack_kernel<T, F, kUnroll, false>;
+    hipLaunchKernelGGL(kernel, dim3((total + per - 1) / per), dim3(kThreads), 0, stream, (const unsigned char *)x,
+                       row_stride, cols, blocks, pitch, total, codes, scales);
     return hipGetLastError();
 }
 
@@ -246,8 +263,10 @@ hipError_t unpack_typed(int64_t rows, int64_t cols, const uint8_t *codes, const 
     const uint32_t blocks = (uint32_t)mx_blocks(cols), pitch = (uint32_t)mx_scale_pitch(cols);
     const uint32_t total = (uint32_t)(rows * blocks);
     constexpr uint32_t per = kThreads / (kMxBlock / kPerLane<T>) * kUnroll;
-    hipLaunchKernelGGL((unpack_kernel<T, F, kUnroll>), dim3((total + per - 1) / per), dim3(kThreads), 0, stream,
-                       codes, scales, cols, blocks, pitch, total, (unsigned char *)x, row_stride);
+    const auto kernel = streamed(x, rows, row_stride, cols, NumTraits<T>::bytes) ? unpack_kernel<T, F, kUnroll, true>
+                                                                                : unpack_kernel<T, F, kUnroll, false>;
+    hipLaunchKernelGGL(kernel, dim3((total + per - 1) / per), dim3(kThreads), 0, stream, codes, scales, cols, blocks,
+                       pitch, total, (unsigned char *)x, row_stride);
     return hipGetLastError();
 }
 

@@ -233,19 +233,19 @@ hipError_t direct(const ProductArgs &p, hipStream_t stream)
 // per 128 k a wavefront issues 32 products (1024 cycles of its matrix core) for 16 operands of 1 KB.  WT = 2,
 // 128 x 128, two workgroups to a compute unit: twice the reads of LDS per product, for products that are too
 // small to fill the chip with large tiles.
-//   - Four buffers of 128 k.  Codes go from memory to LDS without passing registers, four steps ahead, and
-//     from LDS to registers one step ahead, while the products of the step before run: neither is waited for
-//     in steady state.  A wavefront waits for its own loads of the next step only, then for the others at the
-//     step's one barrier.
-//   - A row's 64 bytes of a step lie in LDS as four pieces of 16, piece c at place c ^ (row / 4) % 4: the 16
-//     rows that a quarter of a wavefront reads at once then cover all banks.
-//   - Scales are taken for four steps at a time (16 bytes of a row), a round of four steps ahead; three byte
-//     permutes turn them into one register that holds a lane's scale of each of the four steps, which the
-//     instruction picks by its operand selector.
+//   - Two buffers of 256 k, whole lines of 128 bytes a row (64 bytes at a time ask the caches for twice as
+//     much: 170 against 165 us at 16320 x 4096 x 4096).  Codes go from memory to LDS without passing
+//     registers, two steps of 128 k ahead, and from LDS to registers one step ahead, while the products of
+//     the step before run.
+//   - A row's 128 bytes lie in LDS as eight pieces of 16, piece c at place c ^ (row / 2) % 8: the 16 rows that a
+//     quarter of a wavefront reads at once then cover all banks.
+//   - Scales are taken for four steps at a time (16 bytes of a row); three byte permutes turn them into one
+//     register that holds a lane's scale of each of the four steps, which the instruction picks by its
+//     operand selector.
 // Past the end of k the codes of A are zeros and the scales powers of two; rows past M or N repeat the last
 // one and are not stored.
 
-__device__ inline uint32_t tile_place(uint32_t row, uint32_t piece) { return row * 4 + (piece ^ ((row >> 2) & 3)); }
+__device__ inline uint32_t tile_place(uint32_t row, uint32_t piece) { return row * 8 + (piece ^ ((row >> 1) & 7)); }
 
 template <int Step> __device__ inline v16f product_step(v4u b, v4u a, v16f c, int sb, int sa)
 {
@@ -263,7 +263,7 @@ __device__ inline int scale_bytes(v4u w, uint32_t pick)
 
 // 16 bytes per lane from memory (a common base, an offset per lane) to LDS, where they lie one lane after the
 // other.  Written as an instruction because the compiler would wait for every load under way before each read
-// of LDS; nothing is returned to registers, and wait_loads and the barrier stand before the first read of
+// of LDS (223 against 209 us, before the steps that followed); nothing is returned to registers, and wait_loads and the barrier stand before the first read of
 // what was loaded.  The address in LDS goes by m0, which is put back.
 __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t lds)
 {
@@ -286,10 +286,10 @@ template <Num T, int WT>
 __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(ProductArgs p, int mtiles, int ntiles)
 {
     constexpr int kTile = 64 * WT;
-    constexpr int kBuffer = kTile * 8;                      // 16-byte pieces of a buffer: codes of A, then of B
-    constexpr int kLoads = 2 * WT;                          // a wavefront's loads of a step, 16 rows each
-    __shared__ v4u lds[4 * kBuffer + 2 * kTile];            // then 16 bytes of scales for every row of A and B
-    v4u *const lds_s = lds + 4 * kBuffer;
+    constexpr int kBuffer = kTile * 16;                     // 16-byte pieces of a buffer: codes of A, then of B
+    constexpr int kLoads = 4 * WT;                          // a wavefront's loads of a buffer, 8 rows each
+    __shared__ v4u lds[2 * kBuffer + 2 * kTile];            // then 16 bytes of scales for every row of A and B
+    v4u *const lds_s = lds + 2 * kBuffer;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5;                 // an operand: row r, the h-th 32 of its 64 k
     const int wm = wave >> 1, wn = wave & 1;
@@ -308,19 +308,20 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     const int steps = (p.blocks + 3) / 4;
     const uint8_t *const base_a = (const uint8_t *)p.a + (int64_t)m0 * p.pitch;
     const uint8_t *const base_b = p.b + (int64_t)n0 * p.pitch;
-    const uint32_t piece = (lane & 3) ^ (lane >> 4);        // see tile_place: row / 4 = lane / 16 modulo 4
+    const uint32_t piece = (lane & 7) ^ (4 * (wave & 1) + (lane >> 4));     // see tile_place: row / 2 modulo 8
     uint32_t off[kLoads];
 #pragma unroll
     for (int i = 0; i < kLoads; ++i) {
-        const int row = (4 * (i % WT) + wave) * 16 + (lane >> 2);
-        off[i] = (uint32_t)min(row, (i < WT ? p.M - m0 : p.N - n0) - 1) * p.pitch + 16 * piece;
+        const int row = (4 * (i % (2 * WT)) + wave) * 8 + (lane >> 3);
+        off[i] = (uint32_t)min(row, (i < 2 * WT ? p.M - m0 : p.N - n0) - 1) * p.pitch + 16 * piece;
     }
     const uint32_t put = lds_address(lds) + wave * 1024;
-    auto fetch = [&](int step, int buffer, int which, uint32_t back) {      // 16 rows of A, or (from WT on) of B
-        load_to_lds((which < WT ? base_a : base_b) + step * 64, off[which] - back, put + buffer * kBuffer * 16 + which * 4096);
+    auto fetch = [&](int pair, int buffer, int which, uint32_t back) {      // 8 rows of A, or (from 2 WT on) of B
+        load_to_lds((which < 2 * WT ? base_a : base_b) + pair * 128, off[which] - back,
+                    put + buffer * kBuffer * 16 + which * 4096);
     };
-    // pieces past a row's end are not read: the lane takes the step's first piece, which its row has
-    auto past_end = [&](int step) { return step * 4 + (int)piece < p.blocks ? 0u : 16 * piece; };
+    // pieces past a row's end are not read: the lane takes the pair's first piece, which its row has
+    auto past_end = [&](int pair) { return pair * 8 + (int)piece < p.blocks ? 0u : 16 * piece; };
     auto fetch_scales = [&](int step) {                     // of steps step .. step + 3
 #pragma unroll
         for (int i = 0; i < WT / 2; ++i) {
@@ -344,15 +345,19 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
         }
     };
 
-    const uint32_t lane_at[2] = {tile_place(r, h), tile_place(r, 2 + h)};       // first and second 64 k
+    uint32_t lane_at[2][2];                                 // [step of the pair][first or second 64 k]
+#pragma unroll
+    for (int o = 0; o < 2; ++o)
+#pragma unroll
+        for (int k = 0; k < 2; ++k) lane_at[o][k] = tile_place(r, 4 * o + 2 * k + h);
     struct Operands {
         v4u a[2][WT], b[2][WT];
     };
-    auto read = [&](int buffer, int which, Operands &o) {   // one of 4 WT, those of the first 64 k first
-        const v4u *from = lds + buffer * kBuffer;
-        const int k = which / (2 * WT), i = which % WT;
-        if (which / WT & 1) o.a[k][i] = from[(wm * WT + i) * 128 + lane_at[k]];
-        else o.b[k][i] = from[kTile * 4 + (wn * WT + i) * 128 + lane_at[k]];
+    auto read = [&](int step, int which, Operands &to) {    // one of 4 WT, those of the first 64 k first
+        const v4u *from = lds + (step >> 1 & 1) * kBuffer;
+        const int k = which / (2 * WT), i = which % WT, o = step & 1;
+        if (which / WT & 1) to.a[k][i] = from[(wm * WT + i) * 256 + lane_at[o][k]];
+        else to.b[k][i] = from[kTile * 8 + (wn * WT + i) * 256 + lane_at[o][k]];
     };
     const uint32_t pick = (uint32_t)h | (uint32_t)(4 + h) << 8 | 0x0c0c0000u;
     struct Scales {
@@ -376,16 +381,16 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
 
     Scales scales, later;
     Operands even, odd;
+    const int last_pair = (steps - 1) >> 1;
     fetch_scales(0);
 #pragma unroll
-    for (int s = 0; s < 4; ++s)
-        if (s < steps) {
-            const uint32_t back = past_end(s);
+    for (int q = 0; q < 2; ++q) {
+        const int pair = min(q, last_pair);
+        const uint32_t back = past_end(pair);
 #pragma unroll
-            for (int q = 0; q < kLoads; ++q) fetch(s, s, q, back);
-        }
-    if (steps > 3) wait_loads<3 * kLoads>();
-    else wait_loads<0>();
+        for (int i = 0; i < kLoads; ++i) fetch(pair, q, i, back);
+    }
+    wait_loads<kLoads>();
     __builtin_amdgcn_s_barrier();
 #pragma unroll
     for (int q = 0; q < 4 * WT; ++q) read(0, q, even);
@@ -394,21 +399,25 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
 
     for (int step0 = 0; step0 < steps; step0 += 4) {
         scales = later;
-        // One step.  At its barrier this step's operands are in registers in every wavefront and the next
-        // step's codes in LDS; between the products the next step's operands are read and the codes four
-        // steps on are asked for (the last step's again where there are none: the count of loads under way
-        // stays the same, and nothing reads them).  The order is pinned: a wavefront issues one instruction
-        // at a time, and everything else has to fit between two products.
+        // One step.  Between its products the next step's operands are read.  At the barrier of the second
+        // step of a pair every wavefront has this pair's operands in registers and the next pair's codes in
+        // LDS, and the pair after that is asked for (the last pair again where there is none: nothing reads
+        // it).  The order is pinned: a wavefront issues one instruction at a time, and everything else has to
+        // fit between two products.
         auto one = [&](auto which) {
             constexpr int W = decltype(which)::value;
             const int step = step0 + W;
             if (step >= steps) return;
             Operands &now = W & 1 ? odd : even, &next = W & 1 ? even : odd;
-            wait_loads<2 * kLoads>();
-            __builtin_amdgcn_s_barrier();
-            if (W == 0 && step + 4 < steps) fetch_scales(step + 4);
-            const int ahead = min(step + 4, steps - 1);
-            const uint32_t back = past_end(ahead);
+            int ahead = 0;
+            uint32_t back = 0;
+            if constexpr (W & 1) {
+                wait_loads<0>();
+                __builtin_amdgcn_s_barrier();
+                if (W == 1 && step + 3 < steps) fetch_scales(step + 3);
+                ahead = min((step >> 1) + 2, last_pair);
+                back = past_end(ahead);
+            }
             if (step * 4 + 4 > p.blocks) {
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
@@ -418,19 +427,17 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
                 }
             }
             __builtin_amdgcn_sched_barrier(0);
-            constexpr int kProducts = 2 * WT * WT, kReads = 4 * WT;
+            constexpr int kProducts = 2 * WT * WT, kReads = 4 * WT, kLate = kProducts / 4;
 #pragma unroll
             for (int t = 0; t < kProducts; ++t) {
                 const int k = t / (WT * WT), i = t / WT % WT, j = t % WT;
                 acc[i][j] = product_step<W>(now.b[k][j], now.a[k][i], acc[i][j], scales.b[k][j], scales.a[k][i]);
-                if constexpr (WT == 4) {
-                    if (t < kReads) read((W + 1) & 3, t, next);
-                    if (t >= kReads && (t & 1) == 0) fetch(ahead, W, (t - kReads) >> 1, back);
-                    if (W >= 2 && (t == 19 || t == 27)) read_scales((W - 2) * 2 + (t == 27), later);
-                } else {
-                    read((W + 1) & 3, t, next);
-                    if (t & 1) fetch(ahead, W, t >> 1, back);
-                    if (W >= 2 && t == 6) read_scales(W - 2, later);
+                if constexpr (W & 1) {
+                    if (t < kLoads) fetch(ahead, W >> 1, t, back);
+                    if (WT == 4 ? t >= kLate && t < kLate + kReads : true) read(W + 1, WT == 4 ? t - kLate : t, next);
+                    if (W == 3 && t >= kProducts - WT) read_scales(t - (kProducts - WT), later);
+                } else if (t < kReads) {
+                    read(W + 1, t, next);
                 }
                 __builtin_amdgcn_sched_barrier(0);
             }
@@ -448,7 +455,7 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kPitch = 32 * WT + 4;
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();
-    float *const mine = (float *)(lds + wave * kBuffer);
+    float *const mine = (float *)(lds + wave * (kBuffer / 2));
     const int col = P * (lane % kLanes), n = n0 + wn * 32 * WT + col;
     float bias[P];
 #pragma unroll
@@ -503,8 +510,8 @@ int64_t small_tiles(int M, int N) { return (int64_t)((M + 15) / 16) * ((N + 15) 
 // Which kernel.  Microseconds measured back to back, float results:
 //   - up to 512 tiles of 16 x 16 the chip has room for a workgroup each (1 x 8192 or 300 x 400): a
 //     workgroup per tile, its wavefronts share k.  300 x 300 x 512: 3.4, with 32 x 32 tiles 4.4, 128 x 128 6.7.
-//   - up to 1536, or 4096 where k is one step: 32 x 32 tiles.  8000 x 28 x 2048: 6.4 (16 x 16 9.7, 128 x 128
-//     9.8); 300 x 2048 x 512: 7.9 against 6.9.
+//   - up to 1536, or 4096 where k is one step, unless k is very long: 32 x 32 tiles.  8000 x 28 x 2048: 6.4
+//     (16 x 16 9.7, 128 x 128 9.8); 300 x 2048 x 512: 7.9 against 6.9; 300 x 1000 x 4096: 17.7 against 13.3.
 //   - beyond, tiles of 128 or 256 through LDS, by how many rounds of workgroups they take and what a round
 //     costs (us, K in numbers): 14.5 + 0.0075 K for 256 tiles of 256, 8.5 + 0.0052 K for 512 of 128.
 //     2040 x 2048 x 2048: 14.0 with 128, 25.6 with 256; 32000 x 2048 x 2048: 152 with 128, 121 with 256.
@@ -513,7 +520,7 @@ hipError_t product_typed(const ProductArgs &p, hipStream_t stream)
 {
     const int64_t small = small_tiles(p.M, p.N);
     if (small <= 512) return direct<T, false, 1, 1, 4, 4>(p, stream);
-    if (small <= (p.K <= 128 ? 4096 : 1536)) return direct<T, false, 2, 2, 4, 4>(p, stream);
+    if (small <= (p.K <= 128 ? 4096 : 1536) && small * p.K <= 3000000) return direct<T, false, 2, 2, 4, 4>(p, stream);
     const int64_t large = (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256);
     const int64_t mid = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
     const double cost_large = (double)((large + 255) / 256) * (14.5 + 0.0075 * p.K);

@@ -143,6 +143,20 @@ def test_a_row_longer_than_the_offsets_of_32_bits():
     assert worst <= float(x.abs().max()) * 2.0 ** -6
 
 
+@pytest.mark.parametrize("fmt,dtype", itertools.product(FORMATS, DTYPES))
+def test_tensors_past_the_memory_side_cache(fmt, dtype):
+    """A tensor of more than 256 MB, whose codes and numbers are those of its two halves."""
+    t = DTYPES[dtype]
+    n = (1 << 27) // t.itemsize + (1 << 20)
+    x = torch.empty((2, n), dtype=t, device="cuda").normal_()
+    whole, halves = mgd.mg_mx_pack(x, fmt), [mgd.mg_mx_pack(x[k:k + 1], fmt) for k in range(2)]
+    assert torch.equal(whole.codes, torch.cat([h.codes for h in halves]))
+    assert torch.equal(whole.scales, torch.cat([h.scales for h in halves]))
+    back = mgd.mg_mx_unpack(whole)
+    for k in range(2):
+        assert torch.equal(back[k:k + 1], mgd.mg_mx_unpack(halves[k]))
+
+
 # ---- weight gradients ----
 
 GRADS = [(1, 1, 1, 1), (1, 5, 3, 7), (2, 16, 4, 32), (1, 17, 28, 33), (3, 100, 5, 130), (2, 333, 33, 256),
