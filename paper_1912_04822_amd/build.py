@@ -9,6 +9,9 @@ import sys
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libmolgrid_hip.so")
+# the C++ side of the Python binding (host code only)
+BINDING_SOURCE = os.path.join(CSRC, "mg_binding.cpp")
+BINDING = os.path.join(HERE, "_binding.so")
 # measurement build: the same sources with -DMG_TIMING_AIDS (kernel phases can be switched off
 # to time the rest; such runs write wrong grids, so the release library has none of it)
 LIB_TIMING = os.path.join(HERE, "libmolgrid_hip_timing.so")
@@ -29,6 +32,28 @@ def sources():
     return sorted(glob.glob(os.path.join(CSRC, "*.hip")))
 
 
+def build_binding(verbose: bool = False) -> str:
+    """Compile the C++ side of the Python binding against the installed torch."""
+    import sysconfig
+
+    import torch
+    from torch.utils import cpp_extension
+
+    includes = cpp_extension.include_paths() + [sysconfig.get_paths()["include"]]
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           "-D_GLIBCXX_USE_CXX11_ABI=%d" % int(torch._C._GLIBCXX_USE_CXX11_ABI)]
+    for path in includes:
+        cmd += ["-isystem", path]
+    cmd += [BINDING_SOURCE, "-o", BINDING, "-L" + os.path.join(os.path.dirname(torch.__file__), "lib"),
+            "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    if verbose:
+        print(" ".join(cmd), flush=True)
+    res = subprocess.run(cmd, capture_output=True, text=True)
+    if res.returncode != 0:
+        raise RuntimeError("the binding does not compile:\n" + res.stdout + res.stderr)
+    return BINDING
+
+
 def build_library(verbose: bool = False, timing_aids: bool = False) -> str:
     hipcc = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
     out = LIB_TIMING if timing_aids else LIB
@@ -42,6 +67,8 @@ def build_library(verbose: bool = False, timing_aids: bool = False) -> str:
         raise RuntimeError("hipcc failed:\n" + msgs)
     if verbose and msgs.strip():
         print(msgs)
+    if not timing_aids:
+        build_binding(verbose)
     return out
 
 

@@ -7,6 +7,7 @@ fallback: if the shared library is missing, loading raises.
 from __future__ import annotations
 
 import ctypes
+import importlib.util
 import os
 from typing import Optional
 
@@ -31,7 +32,10 @@ EXPORTS = [
     "mg_mx4_product", "mg_mx4_linear", "mg_mx4_linear_workspace",
 ]
 
+BINDING_PATH = os.path.join(_HERE, "_binding.so")
+
 _lib: Optional[ctypes.CDLL] = None
+_binding = None         # the C++ side of the microscaled-format calls, loaded with the library
 
 
 class MolgridError(RuntimeError):
@@ -117,8 +121,25 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
         L.mg_set_option.argtypes = [ctypes.c_char_p, ci]
         L.mg_time_next_kernel.restype = ci
         L.mg_time_next_kernel.argtypes = [vp, vp]
+        _load_binding(L)
         _lib = L
     return _lib
+
+
+def _load_binding(L) -> None:
+    """Load the C++ side of the binding and hand it the addresses of the library's functions."""
+    global _binding
+    if not os.path.exists(BINDING_PATH):
+        raise FileNotFoundError(
+            "binding not built: %s (run python -m paper_1912_04822_amd.build)" % BINDING_PATH)
+    name = __package__ + "._binding"
+    spec = importlib.util.spec_from_file_location(name, BINDING_PATH)
+    module = importlib.util.module_from_spec(spec)
+    spec.loader.exec_module(module)
+    module.bind(*(ctypes.cast(getattr(L, f), ctypes.c_void_p).value for f in (
+        "mg_mx_pack", "mg_mx_unpack", "mg_mx8_weight_gradient_workspace", "mg_mx8_weight_gradient",
+        "mg_mx4_product", "mg_mx4_linear_workspace", "mg_mx4_linear")))
+    _binding = module
 
 
 def strerror(code: int) -> str:
@@ -594,6 +615,25 @@ def _launch(fn, dev, *args):
         raise MolgridError(rc, fn.__name__)
 
 
+def _native(dev):
+    """The C++ side of the binding, which takes calls on the current device in their common form (dense
+    tensors, new results) and returns None for any other, or None."""
+    if dev < 0 or _raw_stream is None or dev != _current_device():
+        return None
+    if _binding is None:
+        lib()
+    return _binding
+
+
+def _taken(r, name):
+    """Whether the C++ side took a call; raises the library's error."""
+    if r is None:
+        return False
+    if type(r) is int:
+        raise MolgridError(r, name)
+    return True
+
+
 def _workspace_of(fn, like, *sizes):
     """The workspace a call of these sizes needs (bytes from ``fn``), and its size.  A new one for
     every call: calls on several streams, or captured in several graphs, share none."""
@@ -607,6 +647,13 @@ def _workspace_of(fn, like, *sizes):
 def mg_mx_pack(x, format="int8", out: Optional[MXTensor] = None) -> MXTensor:
     """``x`` (float32, float16 or bfloat16; rows along the last dimension, equally far apart) in
     blocks of 32 numbers that share a power of two."""
+    if out is None and format in MX_FORMATS:
+        dev = x.get_device()
+        native = _native(dev)
+        if native is not None:
+            r = native.pack(x, MX_FORMATS[format], dev, _raw_stream(dev))
+            if _taken(r, "mg_mx_pack"):
+                return MXTensor(r[0], r[1], x.shape, format, x.dtype)
     shape = x.shape
     rows, cols, cshape, sshape = _mx_layout(shape, format)
     dtype, stride, dev = _number(x.dtype, "x"), _row_stride(x, "x"), _device(x, "x")
@@ -626,6 +673,13 @@ def mg_mx_pack(x, format="int8", out: Optional[MXTensor] = None) -> MXTensor:
 def mg_mx_unpack(packed: MXTensor, dtype=None, out=None):
     """The numbers ``packed`` stands for, as a tensor of its shape (``dtype``: default its own)."""
     dev = _device(packed.codes, "packed.codes")
+    if out is None and isinstance(packed, MXTensor):
+        native = _native(dev)
+        if native is not None:
+            r = native.unpack(packed.codes, packed.scales, packed.shape, MX_FORMATS.get(packed.format),
+                              NUMBERS.get(dtype or packed.dtype), dev, _raw_stream(dev))
+            if _taken(r, "mg_mx_unpack"):
+                return r
     rows, cols, codes, scales = _mx_pointers(packed, "packed", MX_FORMATS, dev)
     if out is None:
         out = packed.codes.new_empty(packed.shape, dtype=dtype or packed.dtype)
@@ -644,6 +698,14 @@ def mg_mx8_weight_gradient(grad, packed: MXTensor, natoms=None, grad_weight=None
     on y and the 8-bit codes of x [...,E].  ``natoms`` [B] (x of shape [B,N,E]): atoms past it
     count for nothing, whatever their rows hold."""
     dev = grad.get_device()
+    if (grad_weight is None and grad_bias is None and isinstance(packed, MXTensor)
+            and packed.format in ("int8", "e4m3")):
+        native = _native(dev)
+        if native is not None:
+            r = native.gradient(grad, packed.codes, packed.scales, packed.shape, MX_FORMATS[packed.format], natoms,
+                                dev, _raw_stream(dev))
+            if _taken(r, "mg_mx8_weight_gradient"):
+                return r
     rows, E, codes, scales = _mx_pointers(packed, "packed", ("int8", "e4m3"), dev)
     T = grad.shape[-1]
     if tuple(grad.shape[:-1]) != packed.shape[:-1]:
@@ -681,6 +743,14 @@ def _product_out(out, shape, dtype, like, dev):
 def mg_mx4_product(a: MXTensor, b: MXTensor, bias=None, dtype=torch.float32, out=None):
     """``a`` [...,K] times ``b`` [N,K] transposed, plus ``bias`` [N] (float32): [...,N] of ``dtype``."""
     dev = _device(a.codes, "a.codes")
+    if (out is None and isinstance(a, MXTensor) and isinstance(b, MXTensor) and a.format == "e2m1"
+            and b.format == "e2m1"):
+        native = _native(dev)
+        if native is not None:
+            r = native.product(a.codes, a.scales, a.shape, b.codes, b.scales, b.shape, bias, NUMBERS.get(dtype), dev,
+                               _raw_stream(dev))
+            if _taken(r, "mg_mx4_product"):
+                return r
     M, K, ac, asc = _mx_pointers(a, "a", ("e2m1",), dev)
     N, Kb, bc, bsc = _mx_pointers(b, "b", ("e2m1",), dev)
     if K != Kb:
@@ -697,6 +767,12 @@ def mg_mx4_linear(x, weight: MXTensor, bias=None, out=None):
     """``x`` [...,K] (plain numbers, taken to "e2m1" by the call) times ``weight`` [N,K] transposed,
     plus ``bias`` [N] (float32): [...,N] in the type of ``x``."""
     dev = x.get_device()
+    if out is None and isinstance(weight, MXTensor) and weight.format == "e2m1":
+        native = _native(dev)
+        if native is not None:
+            r = native.linear(x, weight.codes, weight.scales, weight.shape, bias, dev, _raw_stream(dev))
+            if _taken(r, "mg_mx4_linear"):
+                return r
     N, K, wc, wsc = _mx_pointers(weight, "weight", ("e2m1",), dev)
     shape = x.shape
     if shape[-1] != K:

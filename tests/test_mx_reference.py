@@ -159,3 +159,19 @@ def test_binding_refuses():
         molgrid.mg_mx4_linear(x, t)                 # eight bits where four are wanted
     with pytest.raises(ValueError):
         molgrid.mg_mx_unpack(t)                     # codes not on the device
+
+
+def test_the_native_side_leaves_other_calls_alone():
+    """Calls that are not of the common form are handed back (None) before anything is touched."""
+    molgrid.lib()
+    b = molgrid._binding
+    x, codes, scales = torch.zeros((4, 40)), torch.zeros((4, 64), dtype=torch.uint8), torch.zeros((4, 4), dtype=torch.uint8)
+    assert b.pack(x, 0, 0, 0) is None and b.pack(None, 0, 0, 0) is None and b.pack(x) is None
+    assert b.pack(x, "int8", 0, 0) is None and b.pack(x, 0, 1 << 70, 0) is None
+    assert b.unpack(codes, scales, (4, 40), 0, 0, 0, 0) is None
+    assert b.unpack(codes, scales, [4, 40], 0, 0, 0, 0) is None
+    assert b.gradient(x, codes, scales, (4, 40), 0, None, 0, 0) is None
+    assert b.product(codes, scales, (4, 40), codes, scales, (4, 40), None, 0, 0, 0) is None
+    assert b.linear(x, codes, scales, (4, 40), None, 0, 0) is None
+    with pytest.raises(TypeError):
+        b.bind(1)
