@@ -1,24 +1,29 @@
 // Weight gradient of a linear map from the 8-bit codes of its input (formats: mg_mx.h):
 //     dW[t][e] = sum over live rows m of G[m][t] X[m][e],     db[t] = sum over live rows of G[m][t].
-// X is M x E codes and by far the largest operand, T (channels) is small: what bounds the kernel is
-// reading the codes once.  A wavefront therefore keeps a 32 x 256 piece of dW (16 to 64 channels) in its
-// accumulators and walks down the rows, 32 at a time, with v_mfma_f32_16x16x32_bf16.
+// X is M x E codes and by far the largest operand, T (channels) is small: the kernel is bound by reading the
+// codes once and by taking them apart.  A wavefront keeps a piece of dW, 32 channels by 128 columns (up to 16
+// channels: 16 by 256), in its accumulators and walks down the rows, 32 at a time, with
+// v_mfma_f32_16x16x32_bf16.
 //   - The sum runs over rows, so the matrix operands want 8 consecutive ROWS of one column per lane
 //     while memory holds rows.  Which column of dW a matrix column stands for is free: lane c takes
-//     columns 16c..16c+15, 16 bytes of codes per row, and byte j of its 8 rows is its operand of the j-th
-//     of sixteen products.  No transpose through LDS, and the results of the products are neighbouring
-//     numbers of dW.  Channels likewise: a lane loads 2 (4) neighbours of a row for 2 (4) operands.
-//   - A wavefront can have 63 loads under way: loads are as wide as can be (17 a step of 32 rows and 256
-//     columns), the scales come in one word per lane and go to the lanes that need them by an exchange.
-//   - A code times its power of two is exact in bfloat16 (at most 8 significant bits); blocks whose
+//     columns 8c..8c+7 (16c..), 8 (16) bytes of codes a row, and byte j of its 8 rows is its operand of the
+//     j-th of 8 (16) products.  No transpose through LDS, and the results of the products are neighbouring
+//     numbers of dW.  Channels likewise: a lane loads 2 neighbours of a row for 2 operands.
+//   - A wavefront can have 63 loads under way: loads are as wide as can be, 17 a step, and the scales come in
+//     one word per lane and go to the lanes that need them by an exchange.  (24 loads per 16 rows: 19.5 and 39
+//     us below.)
+//   - A code times its power of two is exact in bfloat16 (at most 8 significant bits); int8 blocks whose
 //     scale byte is 0 (magnitudes below 2^-120) count as zero.  A float gradient is cut into three
 //     bfloat16 pieces (8 + 8 + 8 bits, exact), a half one into two, so that the products are exact and
 //     only their sum, in float, rounds.
 //   - Rows that are not live (past natoms[b], or past the end) are zeroed in both operands by a mask of
-//     the 16 rows, so that whatever they hold counts for nothing.
-//   - The rows are split over workgroups and the four wavefronts of each; partial sums are added in a
+//     the 32 rows, so that whatever they hold counts for nothing.
+//   - The rows are split over workgroups and the eight wavefronts of each; partial sums are added in a
 //     fixed order (LDS, then a second kernel over the workgroups' sums), so the same call gives the same
 //     bits every time.
+// Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 17.3 us (38 MB: 2.2 TB/s; the
+// first kernel 14.5, 3 to 4 steps a wavefront and their vector instructions, 5 a code); 96000 live of 128000 x
+// 1000 e4m3, 28 of bfloat16 33 us (110 MB: 3.3 TB/s); 512000 x 256 e4m3 36 us (4.5 TB/s).
 #include "mg_common.h"
 #include "mg_mx.h"
 #include "mg_mx_ops.h"
@@ -153,11 +158,11 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
 
     auto compute = [&](Step<T, Q, Words> &r) {
         if (r.live == 0) return;
-        float s[8], off[8];
+        float s[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t w = (uint32_t)__builtin_amdgcn_ds_bpermute(scale_from + 4 * i, (int)r.scale);
-            s[i] = mx_bits(((w >> shift) & 255u) << 23);        // S = 255: infinity, times code 0
+            s[i] = mx_bits(((w >> shift) & 255u) << 23);        // S = 255: infinity; times code 0, or read as a scale, NaN
         }
         if (r.live != 0xffffffffu) {
             const uint32_t mine = r.live >> (8 * g);
@@ -171,8 +176,6 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
                 for (int q = 0; q < Q; ++q) r.g[i][q] = on ? r.g[i][q] : (E)0.0f;
             }
         }
-#pragma unroll
-        for (int i = 0; i < 8; ++i) off[i] = -128.0f * s[i];
         v8bf gp[Q][kPieces<T>];
 #pragma unroll
         for (int q = 0; q < Q; ++q) {
@@ -198,15 +201,12 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
             // this lane's 8 rows of 4 columns, as 4 operands
             v4u x[4];
             if constexpr (F == Mx::INT8) {
-                // bytes as q + 128, which one conversion takes; (q + 128) s - 128 s = q s is exact
 #pragma unroll
-                for (int i = 0; i < 8; i += 2) {
-                    const uint32_t u = r.code[i][w] ^ 0x80808080u, v = r.code[i + 1][w] ^ 0x80808080u;
+                for (int i = 0; i < 8; i += 2)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
-                        x[j][i / 2] = pair_hi(fmaf((float)((v >> (8 * j)) & 255u), s[i + 1], off[i + 1]),
-                                              fmaf((float)((u >> (8 * j)) & 255u), s[i], off[i]));
-                }
+                        x[j][i / 2] = pair_hi((float)(int)(int8_t)(r.code[i + 1][w] >> (8 * j)) * s[i + 1],
+                                              (float)(int)(int8_t)(r.code[i][w] >> (8 * j)) * s[i]);
             } else {
                 // two columns of a row at a time, then two rows of each
 #pragma unroll
@@ -354,7 +354,9 @@ __global__ __launch_bounds__(kSumThreads) void gradient_sum_kernel(GradientArgs 
     if (e + 3 < a.E) to[3] = v.w;
 }
 
-// Channels a lane takes (of the gradient, in one load) and words of codes.
+// Channels a lane takes (of the gradient, in one load) and words of codes: what leaves room for two wavefronts
+// per SIMD (241 registers).  32 channels by 256 columns with one wavefront per SIMD: 20.9 us where this takes
+// 17.3, 31.7 where it takes 33; 64 by 64: 22.5 against 22.6 at 100 channels, and registers in scratch.
 int lane_channels(int64_t T) { return T > 16 ? 2 : 1; }
 int lane_words(int64_t T, int64_t pitch) { return T > 16 ? 2 : pitch > 64 ? 4 : 1; }
 
@@ -364,8 +366,9 @@ int64_t gradient_tiles(int64_t T, int64_t pitch)
     return ((pitch + cols - 1) / cols) * ((T + chans - 1) / chans);
 }
 
-// Enough workgroups to fill the chip, but at least a step of 32 rows per wavefront, as every split costs a
-// write and a read of T x E sums.
+// A workgroup per compute unit (512: 24.0 instead of 17.4 us, 192: 18.9), but at least a step of 32 rows per
+// wavefront (4 steps: 14.2 instead of 9.1 us at 2040 rows), as every split costs a write and a read of T x E
+// sums.
 constexpr int kWantGroups = 256;
 int gradient_splits(int64_t M, int64_t T, int64_t E)
 {

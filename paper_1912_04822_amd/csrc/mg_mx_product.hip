@@ -6,6 +6,10 @@
 // Products of elements and scales are exact; sums are in float.
 //
 // The operands are given as (B, A), so a lane's four results are 4 neighbouring n of one row m of C.
+//
+// Measured: 16320 x 4096 x 4096 into bfloat16 160 us (3.4 PFLOP/s; of it 27 us for a quarter of k and about 57
+// that do not depend on k: 134 MB of results, four rounds of workgroups); 2040 x 509 x 1000 7.6; plain rows of
+// 102000 x 256 floats to 28 columns 23.4 (116 MB: 5.0 TB/s); one row by 4096 x 4096 6.0 (8.9 MB of weights).
 #include <type_traits>
 
 #include "mg_common.h"
