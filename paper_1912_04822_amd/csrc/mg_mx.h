@@ -77,11 +77,91 @@ template <int Sel> __device__ inline uint32_t mx_encode_pair(uint32_t old, float
     return __builtin_amdgcn_cvt_scalef32_pk_fp4_f32(old, a, b, 1.0f, Sel);
 }
 
-// One number of a row's storage type as float, and back (saturating: a finite value past the largest
-// finite number of the type becomes that number, as the block's scale can lie a step above it).
+// The storage types of plain numbers.
 template <Num T> struct NumTraits;
 template <> struct NumTraits<Num::F32> { using type = float; static constexpr int bytes = 4; };
 template <> struct NumTraits<Num::F16> { using type = _Float16; static constexpr int bytes = 2; };
 template <> struct NumTraits<Num::BF16> { using type = __bf16; static constexpr int bytes = 2; };
+
+using v4u = __attribute__((ext_vector_type(4))) uint32_t;
+
+// Numbers in 16 bytes, and how many lanes that hold so many share a block.
+template <Num T> constexpr int kPerLane = 16 / NumTraits<T>::bytes;
+template <Num T> constexpr int kBlockLanes = kMxBlock / kPerLane<T>;
+
+// 16 bytes from an address that need only be aligned to its element (the hardware takes any).
+__device__ inline v4u load16(const void *p)
+{
+    v4u v;
+    __builtin_memcpy(&v, p, 16);
+    return v;
+}
+
+template <Num T> __device__ inline void widen(v4u w, float *f)
+{
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        if constexpr (T == Num::F32) {
+            f[i] = mx_bits(w[i]);
+        } else if constexpr (T == Num::BF16) {
+            f[2 * i] = mx_bits(w[i] << 16);
+            f[2 * i + 1] = mx_bits(w[i] & 0xffff0000u);
+        } else {
+            f[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
+            f[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
+        }
+    }
+}
+
+// The numbers of a row from column c on that 16 bytes hold; zeros past the row's end.
+template <Num T> __device__ inline v4u load_row(const void *row, int64_t c, int64_t cols)
+{
+    using E = typename NumTraits<T>::type;
+    const E *p = (const E *)row + c;
+    if (c + kPerLane<T> <= cols) return load16(p);
+    if (c >= cols) return v4u{0, 0, 0, 0};
+    E e[kPerLane<T>];
+#pragma unroll
+    for (int i = 0; i < kPerLane<T>; ++i) e[i] = c + i < cols ? p[i] : (E)0.0f;
+    v4u v;
+    __builtin_memcpy(&v, e, 16);
+    return v;
+}
+
+// Largest of the lanes that share a block (8 or 4 neighbours): xor 1, xor 2 within a quad, then the
+// mirror image within 8 lanes.
+template <int Lanes> __device__ inline uint32_t block_max(uint32_t v)
+{
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));     // quad_perm 1,0,3,2
+    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));     // quad_perm 2,3,0,1
+    if constexpr (Lanes == 8)
+        v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));   // row_half_mirror
+    return v;
+}
+
+// This lane's numbers divided by its block's scale (zeros where the block is not finite); the shared byte.
+template <Mx F, Num T> __device__ inline uint32_t scale_block(float *f)
+{
+    uint32_t m = 0;
+#pragma unroll
+    for (int i = 0; i < kPerLane<T>; ++i) m = max(m, mx_word(f[i]) & 0x7fffffffu);
+    const uint32_t s = mx_shared<F>(block_max<kBlockLanes<T>>(m));
+    const float inv = mx_inverse(s);
+#pragma unroll
+    for (int i = 0; i < kPerLane<T>; ++i) f[i] = s == 255u ? 0.0f : f[i] * inv;
+    return s;
+}
+
+// This lane's elements in 4 bits: 16 bits of 4, a word of 8.
+template <Num T> __device__ inline uint32_t encode_e2m1(const float *f)
+{
+    uint32_t w = mx_encode_pair<0>(0u, f[0], f[1]);
+    w = mx_encode_pair<1>(w, f[2], f[3]);
+    if constexpr (kPerLane<T> == 8) {
+        w = mx_encode_pair<2>(w, f[4], f[5]);
+        w = mx_encode_pair<3>(w, f[6], f[7]);
+    }
+    return w;
+}
 
 }  // namespace mg

@@ -36,7 +36,6 @@ constexpr int kWaves = 8, kThreads = 64 * kWaves;
 constexpr int kRows = 32;               // rows of one step
 constexpr int kDepth = 2;               // steps a wavefront holds: one it works on, the rest under way
 
-using v4u = __attribute__((ext_vector_type(4))) uint32_t;
 using v8bf = __attribute__((ext_vector_type(8))) __bf16;
 using v4f = __attribute__((ext_vector_type(4))) float;
 

@@ -17,15 +17,6 @@ namespace {
 
 constexpr int kThreads = 256;
 
-using v4u = __attribute__((ext_vector_type(4))) uint32_t;
-
-// 16 bytes from an address that need only be aligned to its element (the hardware takes any).
-__device__ inline v4u load16(const void *p)
-{
-    v4u v;
-    __builtin_memcpy(&v, p, 16);
-    return v;
-}
 __device__ inline void store16(void *p, v4u v) { __builtin_memcpy(p, &v, 16); }
 
 // A tensor that is larger than the memory-side cache is not found there by whoever comes next: it is read or
@@ -37,24 +28,6 @@ bool streamed(const void *p, int64_t rows, int64_t row_stride, int64_t cols, int
 {
     return rows * cols * bytes > kMemoryCacheBytes && ((uintptr_t)p & 15) == 0 &&
            (rows == 1 || row_stride * bytes % 16 == 0);
-}
-
-template <Num T> constexpr int kPerLane = 16 / NumTraits<T>::bytes;
-
-template <Num T> __device__ inline void widen(v4u w, float *f)
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (T == Num::F32) {
-            f[i] = mx_bits(w[i]);
-        } else if constexpr (T == Num::BF16) {
-            f[2 * i] = mx_bits(w[i] << 16);
-            f[2 * i + 1] = mx_bits(w[i] & 0xffff0000u);
-        } else {
-            f[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
-            f[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
-        }
-    }
 }
 
 template <Num T> __device__ inline v4u narrow(const float *f)
@@ -71,17 +44,6 @@ template <Num T> __device__ inline v4u narrow(const float *f)
         }
     }
     return w;
-}
-
-// Largest of the lanes that share a block (8 or 4 neighbours): xor 1, xor 2 within a quad, then the
-// mirror image within 8 lanes.
-template <int Lanes> __device__ inline uint32_t block_max(uint32_t v)
-{
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0xb1, 0xf, 0xf, true));     // quad_perm 1,0,3,2
-    v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x4e, 0xf, 0xf, true));     // quad_perm 2,3,0,1
-    if constexpr (Lanes == 8)
-        v = max(v, (uint32_t)__builtin_amdgcn_update_dpp(0, (int)v, 0x141, 0xf, 0xf, true));   // row_half_mirror
-    return v;
 }
 
 // Blocks are counted along the scale rows, whose length is a multiple of four: those past a row's last
@@ -107,45 +69,24 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const unsigned char *x, 
         raw[u] = v4u{0, 0, 0, 0};
         if (g < total && blk[u] < blocks) {
             const int64_t c = (int64_t)blk[u] * kMxBlock + sub * P;
-            const unsigned char *p = x + ((int64_t)row[u] * row_stride + c) * NumTraits<T>::bytes;
-            if (c + P <= cols) {
-                if constexpr (Stream) raw[u] = __builtin_nontemporal_load((const v4u *)p);
-                else raw[u] = load16(p);
-            } else if (c < cols) {                          // the end of a row
-                using E = typename NumTraits<T>::type;
-                E e[P];
-#pragma unroll
-                for (int i = 0; i < P; ++i) e[i] = c + i < cols ? ((const E *)p)[i] : (E)0.0f;
-                __builtin_memcpy(&raw[u], e, 16);
-            }
+            const unsigned char *p = x + (int64_t)row[u] * row_stride * NumTraits<T>::bytes;
+            if (Stream && c + P <= cols) raw[u] = __builtin_nontemporal_load((const v4u *)(p + c * NumTraits<T>::bytes));
+            else raw[u] = load_row<T>(p, c, cols);
         }
     }
 #pragma unroll
     for (int u = 0; u < Unroll; ++u) {
         float f[P];
         widen<T>(raw[u], f);
-        uint32_t m = 0;
-#pragma unroll
-        for (int i = 0; i < P; ++i) m = max(m, mx_word(f[i]) & 0x7fffffffu);
-        m = block_max<L>(m);
-        const uint32_t s = mx_shared<F>(m);
-        const float inv = mx_inverse(s);
-#pragma unroll
-        for (int i = 0; i < P; ++i) f[i] = s == 255u ? 0.0f : f[i] * inv;
+        const uint32_t s = scale_block<F, T>(f);
         if (at[u] >= total) continue;
         if (sub == 0) scales[at[u]] = blk[u] < blocks ? (uint8_t)s : (uint8_t)0;
         if (blk[u] >= blocks) continue;
         const int64_t to = ((int64_t)row[u] * blocks + blk[u]) * L + sub;       // in units of P elements
         if constexpr (F == Mx::E2M1) {
-            uint32_t w = mx_encode_pair<0>(0u, f[0], f[1]);
-            w = mx_encode_pair<1>(w, f[2], f[3]);
-            if constexpr (P == 8) {
-                w = mx_encode_pair<2>(w, f[4], f[5]);
-                w = mx_encode_pair<3>(w, f[6], f[7]);
-                ((uint32_t *)codes)[to] = w;
-            } else {
-                ((uint16_t *)codes)[to] = (uint16_t)w;
-            }
+            const uint32_t w = encode_e2m1<T>(f);
+            if constexpr (P == 8) ((uint32_t *)codes)[to] = w;
+            else ((uint16_t *)codes)[to] = (uint16_t)w;
         } else if constexpr (P == 8) {
             ((uint2 *)codes)[to] = make_uint2(mx_encode4<F>(f), mx_encode4<F>(f + 4));
         } else {

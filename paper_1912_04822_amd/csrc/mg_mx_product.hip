@@ -20,7 +20,6 @@ namespace mg {
 
 namespace {
 
-using v4u = __attribute__((ext_vector_type(4))) uint32_t;
 using v8i = __attribute__((ext_vector_type(8))) int;
 using v4f = __attribute__((ext_vector_type(4))) float;
 using v16f = __attribute__((ext_vector_type(16))) float;
@@ -67,22 +66,6 @@ __device__ inline Operand load_block(const uint8_t *codes, const uint8_t *scales
     return o;
 }
 
-template <Num T> __device__ inline void widen16(v4u w, float *f)        // 16 bytes of plain numbers
-{
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        if constexpr (T == Num::F32) {
-            f[i] = mx_bits(w[i]);
-        } else if constexpr (T == Num::BF16) {
-            f[2 * i] = mx_bits(w[i] << 16);
-            f[2 * i + 1] = mx_bits(w[i] & 0xffff0000u);
-        } else {
-            f[2 * i] = (float)__builtin_bit_cast(_Float16, (uint16_t)w[i]);
-            f[2 * i + 1] = (float)__builtin_bit_cast(_Float16, (uint16_t)(w[i] >> 16));
-        }
-    }
-}
-
 // Block `blk` of a row of plain numbers, taken to e2m1 in this lane.
 template <Num T>
 __device__ inline Operand quantise_block(const ProductArgs &p, uint32_t row, int blk)
@@ -97,7 +80,7 @@ __device__ inline Operand quantise_block(const ProductArgs &p, uint32_t row, int
         for (int i = 0; i < kMxBlock / P; ++i) {
             v4u w;
             __builtin_memcpy(&w, x + i * P, 16);
-            widen16<T>(w, f + i * P);
+            widen<T>(w, f + i * P);
         }
     } else {
 #pragma unroll
@@ -153,7 +136,10 @@ __device__ inline void store_results(const ProductArgs &p, int m, int n, v4f v)
 
 // Operands straight from memory.  A wavefront holds RM x RN tiles of 16 x 16; the KW wavefronts of a
 // group share a tile and split k between them (their sums meet in LDS), the others lie along m.  Two steps'
-// operands are asked for at a time.
+// operands are asked for at a time.  Plain numbers are read by the lane that wants them, 128 bytes of a row in
+// 16-byte loads; read as they lie by neighbouring lanes and exchanged through LDS they take 26.0 instead of 28.7
+// us from memory at 102000 x 256 floats, but 20.6 instead of 13.9 at 8000 x 1000 and 14.2 instead of 12.8 at 8000
+// x 1024 by 64 columns.
 template <Num T, bool Plain, int RM, int RN, int Waves, int KW>
 __global__ __launch_bounds__(64 * Waves) void product_kernel(ProductArgs p)
 {
