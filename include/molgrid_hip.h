@@ -331,8 +331,8 @@ int mg_mx_pack(int format, int dtype, int64_t rows, int64_t cols, const void *x,
                int64_t row_stride, uint8_t *codes, uint8_t *scales, void *stream);
 
 /*
- * Codes into numbers, rounded once to dtype (exact but for MG_F16 outside its
- * range); a finite value past the largest finite number of dtype becomes that
+ * Codes into numbers, rounded once to dtype (exact within the normal range of
+ * dtype); a finite value past the largest finite number of dtype becomes that
  * number.  Nothing between a row's end and the next row is written.
  */
 int mg_mx_unpack(int format, int dtype, int64_t rows, int64_t cols, const uint8_t *codes,
@@ -345,7 +345,8 @@ int mg_mx_unpack(int format, int dtype, int64_t rows, int64_t cols, const uint8_
  *     grad_bias[t]      = sum_{b, a < natoms[b]} grad[b][a][t]
  * grad: B*N rows of T numbers, grad_stride >= T elements apart; grad_weight
  * [T][E] and grad_bias [T] (may be NULL) float, written.  natoms [B] or NULL
- * (all N): rows past it count for nothing, whatever they hold.  Codes and
+ * (all N; a count below 0 is taken as 0, above N as N): rows past it count for
+ * nothing, whatever they hold.  Codes and
  * gradients enter exactly (blocks of magnitudes below 2^-120 as zero), sums
  * are float in a fixed order.  B*N < 2^31-255, T <= 65535, E <= 2^20,
  * grad_stride <= 2^26 (else MG_ESHAPE).  The workspace (32-byte aligned) is scratch.

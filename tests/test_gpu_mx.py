@@ -194,6 +194,63 @@ def test_weight_gradient(fmt, dtype, size, ragged):
     assert torch.equal(again[0], dw) and torch.equal(again[1], db)     # the same bits every time
 
 
+def test_counts_of_no_atoms_and_out_of_range():
+    x = mgd.mg_mx_pack(rng_tensor((3, 40, 70), torch.float32, 11).cuda(), "e4m3")
+    g = rng_tensor((3, 40, 20), torch.float32, 12).cuda()
+    count = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")
+    for out in mgd.mg_mx8_weight_gradient(g, x, natoms=count(0, 0, 0)):
+        assert not out.any()
+    a, b = mgd.mg_mx8_weight_gradient(g, x, natoms=count(-5, 1000, 7)), mgd.mg_mx8_weight_gradient(g, x, natoms=count(0, 40, 7))
+    assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+def test_both_sides_of_the_binding_agree():
+    """Calls of the common form go through C++, results given in advance through Python: the same bits."""
+    x = rng_tensor((5, 60, 100), torch.bfloat16, 13).cuda()
+    g = rng_tensor((5, 60, 9), torch.float16, 14).cuda()
+    w = mgd.mg_mx_pack(rng_tensor((50, 100), torch.float32, 15).cuda(), "e2m1")
+    bias = rng_tensor((50,), torch.float32, 16).cuda()
+    for fmt in FORMATS:
+        a = mgd.mg_mx_pack(x, fmt)
+        b = mgd.mg_mx_pack(x, fmt, out=mgd.MXTensor(torch.empty_like(a.codes), torch.empty_like(a.scales), x.shape, fmt))
+        assert torch.equal(a.codes, b.codes) and torch.equal(a.scales, b.scales) and a.dtype == b.dtype == x.dtype
+        assert torch.equal(mgd.mg_mx_unpack(a), mgd.mg_mx_unpack(a, out=torch.empty_like(x)))
+        if fmt != "e2m1":
+            dw, db = mgd.mg_mx8_weight_gradient(g, a)
+            ew, eb = mgd.mg_mx8_weight_gradient(g, a, grad_weight=torch.empty_like(dw), grad_bias=torch.empty_like(db))
+            assert torch.equal(dw, ew) and torch.equal(db, eb)
+    y = mgd.mg_mx4_linear(x, w, bias)
+    assert torch.equal(y, mgd.mg_mx4_linear(x, w, bias, out=torch.empty_like(y)))
+    p = mgd.mg_mx4_product(a, w, bias, dtype=x.dtype)
+    assert torch.equal(p, y) and torch.equal(p, mgd.mg_mx4_product(a, w, bias, out=torch.empty_like(y)))
+
+
+def test_device_calls_refuse_what_does_not_fit():
+    x = torch.zeros((4, 40), device="cuda")
+    a, w = mgd.mg_mx_pack(x), mgd.mg_mx_pack(x, "e2m1")
+    bad = mgd.MXTensor(a.codes, a.scales, (4, 70), "int8")
+    cpu = mgd.MXTensor(a.codes.cpu(), a.scales.cpu(), (4, 40), "int8")
+    for call in (lambda: mgd.mg_mx_pack(x.double()), lambda: mgd.mg_mx_unpack(a, dtype=torch.float64),
+                 lambda: mgd.mg_mx8_weight_gradient(x.double(), a), lambda: mgd.mg_mx4_product(w, w, dtype=torch.int32),
+                 lambda: mgd.mg_mx4_linear(x, w, bias=torch.zeros(4, device="cuda", dtype=torch.float16)),
+                 lambda: mgd.mg_mx8_weight_gradient(torch.zeros((1, 4, 3), device="cuda"),
+                                                    mgd.MXTensor(a.codes, a.scales, (1, 4, 40), "int8"),
+                                                    natoms=torch.zeros(1, device="cuda"))):
+        with pytest.raises(TypeError):
+            call()
+    for call in (lambda: mgd.mg_mx_pack(x, "int4"), lambda: mgd.mg_mx_unpack(bad), lambda: mgd.mg_mx_unpack(cpu),
+                 lambda: mgd.mg_mx_pack(x.t()[::2]), lambda: mgd.mg_mx8_weight_gradient(x, w),
+                 lambda: mgd.mg_mx8_weight_gradient(x[:3], a), lambda: mgd.mg_mx4_product(a, w),
+                 lambda: mgd.mg_mx4_linear(x[:, :39], w), lambda: mgd.mg_mx4_linear(x, w, bias=torch.zeros(5, device="cuda")),
+                 lambda: mgd.mg_mx8_weight_gradient(x, a, natoms=torch.zeros(4, dtype=torch.int32, device="cuda")),
+                 lambda: mgd.mg_mx4_linear(x, w, out=torch.zeros((4, 5), device="cuda"))):
+        with pytest.raises(ValueError):
+            call()
+    for call in (lambda: mgd.mg_mx_pack(x[:0]), lambda: mgd.mg_mx4_linear(x[:0], w)):
+        with pytest.raises(mgd.MolgridError):
+            call()
+
+
 def test_weight_gradient_of_strided_gradients_and_into_given_arrays():
     x = mgd.mg_mx_pack(rng_tensor((2, 70, 48), torch.float32, 1).cuda())
     wide = rng_tensor((2, 70, 40), torch.float32, 2).cuda()
