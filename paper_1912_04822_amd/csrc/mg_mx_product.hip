@@ -7,8 +7,8 @@
 //
 // The operands are given as (B, A), so a lane's four results are 4 neighbouring n of one row m of C.
 //
-// Measured: 16320 x 4096 x 4096 into bfloat16 160 us (3.4 PFLOP/s; of it 27 us for a quarter of k and about 57
-// that do not depend on k: 134 MB of results, four rounds of workgroups); 2040 x 509 x 1000 7.6; plain rows of
+// Measured: 16320 x 4096 x 4096 into bfloat16 153 us (3.6 PFLOP/s; of it 28 us for a quarter of k and about 40
+// that do not depend on k: 134 MB of results, four rounds of workgroups); 2040 x 509 x 1000 7.2; plain rows of
 // 102000 x 256 floats to 28 columns 23.4 (116 MB: 5.0 TB/s); one row by 4096 x 4096 6.0 (8.9 MB of weights).
 #include <type_traits>
 
@@ -439,14 +439,17 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     }
 
     // A wavefront turns its results through LDS, 32 rows of 32 WT at a time (rows 16 bytes further apart, so
-    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch.  Kept short: a small
-    // product runs through this code once, and waits for it to come from memory.
+    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch, past the caches where they
+    // are aligned: 4096 x 4096 x 1024 into bfloat16 takes 16.9 us so and 24.2 with ordinary stores, 31.9 and 37.0
+    // together with a kernel that reads the result.  Kept short: a small product runs through this code once, and
+    // waits for it to come from memory.
     using E = typename NumTraits<T>::type;
     constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kPitch = 32 * WT + 4;
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();
     float *const mine = (float *)(lds + wave * (kBuffer / 2));
     const int col = P * (lane % kLanes), n = n0 + wn * 32 * WT + col;
+    const bool aligned = (((uintptr_t)p.c | (uintptr_t)(p.c_stride * sizeof(E))) & 15) == 0;
     float bias[P];
 #pragma unroll
     for (int e = 0; e < P; ++e) bias[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
@@ -475,7 +478,10 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
             if (m >= p.M) continue;
             E *to = (E *)p.c + (int64_t)m * p.c_stride + n;
             if (n + P <= p.N) {
-                __builtin_memcpy(to, e, 16);
+                v4u v;
+                __builtin_memcpy(&v, e, 16);
+                if (aligned) __builtin_nontemporal_store(v, (v4u *)to);
+                else __builtin_memcpy(to, e, 16);
             } else {
 #pragma unroll
                 for (int d = 0; d < P; ++d)
@@ -501,20 +507,21 @@ int64_t small_tiles(int M, int N) { return (int64_t)((M + 15) / 16) * ((N + 15) 
 //   - up to 512 tiles of 16 x 16 the chip has room for a workgroup each (1 x 8192 or 300 x 400): a
 //     workgroup per tile, its wavefronts share k.  300 x 300 x 512: 3.4, with 32 x 32 tiles 4.4, 128 x 128 6.7.
 //   - up to 1536, or 4096 where k is one step, unless k is very long: 32 x 32 tiles.  8000 x 28 x 2048: 6.4
-//     (16 x 16 9.7, 128 x 128 9.8); 300 x 2048 x 512: 7.9 against 6.9; 300 x 1000 x 4096: 17.7 against 13.3.
+//     (16 x 16 9.7, 128 x 128 9.8), x 4096: 9.9 against 12.9; 300 x 2048 x 512: 7.9 against 6.9; 300 x 1000 x
+//     4096: 17.7 against 13.3.
 //   - beyond, tiles of 128 or 256 through LDS, by how many rounds of workgroups they take and what a round
-//     costs (us, K in numbers): 14.5 + 0.0075 K for 256 tiles of 256, 8.5 + 0.0052 K for 512 of 128.
-//     2040 x 2048 x 2048: 14.0 with 128, 25.6 with 256; 32000 x 2048 x 2048: 152 with 128, 121 with 256.
+//     costs (us, K in numbers): 11 + 0.0075 K for 256 tiles of 256, 4 + 0.0045 K for 512 of 128.
+//     2040 x 2048 x 2048: 10.8 with 128, 22.5 with 256; 8000 x 2048 x 4096: 48.7 with 128, 44.7 with 256.
 template <Num T>
 hipError_t product_typed(const ProductArgs &p, hipStream_t stream)
 {
     const int64_t small = small_tiles(p.M, p.N);
     if (small <= 512) return direct<T, false, 1, 1, 4, 4>(p, stream);
-    if (small <= (p.K <= 128 ? 4096 : 1536) && small * p.K <= 3000000) return direct<T, false, 2, 2, 4, 4>(p, stream);
+    if (small <= (p.K <= 128 ? 4096 : 1536) && small * p.K <= 4500000) return direct<T, false, 2, 2, 4, 4>(p, stream);
     const int64_t large = (int64_t)((p.M + 255) / 256) * ((p.N + 255) / 256);
     const int64_t mid = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
-    const double cost_large = (double)((large + 255) / 256) * (14.5 + 0.0075 * p.K);
-    const double cost_mid = std::max(1.0, (double)mid / 512) * (8.5 + 0.0052 * p.K);
+    const double cost_large = (double)((large + 255) / 256) * (11.0 + 0.0075 * p.K);
+    const double cost_mid = std::max(1.0, (double)mid / 512) * (4.0 + 0.0045 * p.K);
     return cost_large < cost_mid ? tiled<T, 4>(p, stream) : tiled<T, 2>(p, stream);
 }
 
