@@ -1,8 +1,8 @@
 // Products of matrices in 4 bits (e2m1 elements, formats: mg_mx.h):
 //     C[m][n] = sum_k A[m][k] B[n][k] + bias[n]
-// with v_mfma_scale_f32_16x16x128_f8f6f4.  An operand of that instruction is 32 consecutive k of one row
-// per lane (row = lane % 16, group of 32 = lane / 16) with that lane's scale byte: exactly a block of the
-// format, so 16 bytes of codes and one byte of scales go from memory to the matrix cores as they lie.
+// with v_mfma_scale_f32_16x16x128_f8f6f4 and 32x32x64.  An operand of these is 32 consecutive k of one row per
+// lane (row = lane % 16 or 32, group of 32 = lane / 16 or 32) with that lane's scale byte: exactly a block of
+// the format, so 16 bytes of codes and one byte of scales go from memory to the matrix cores as they lie.
 // Products of elements and scales are exact; sums are in float.
 //
 // The operands are given as (B, A), so a lane's four results are 4 neighbouring n of one row m of C.
@@ -253,8 +253,9 @@ __device__ inline int scale_bytes(v4u w, uint32_t pick)
 
 // 16 bytes per lane from memory (a common base, an offset per lane) to LDS, where they lie one lane after the
 // other.  Written as an instruction because the compiler would wait for every load under way before each read
-// of LDS (223 against 209 us, before the steps that followed); nothing is returned to registers, and wait_loads and the barrier stand before the first read of
-// what was loaded.  The address in LDS goes by m0, which is put back.
+// of LDS (223 against 209 us, before the steps that followed); nothing is returned to registers, and wait_loads
+// and the barrier stand before the first read of what was loaded.  The address in LDS goes by m0, which is put
+// back.
 __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_t lds)
 {
     uint32_t m0;

@@ -17,6 +17,7 @@ _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libmolgrid_hip.so")
 
 MG_OK = 0
+MG_ESHAPE = -2
 MG_EWORKSPACE = -4
 EXPORTS = [
     "mg_gridmaker_create", "mg_gridmaker_create_subgrids", "mg_gridmaker_subgrids_per_side",
@@ -600,6 +601,12 @@ def _row_stride(t, name):
     return step
 
 
+def _fits(name, *sizes):
+    """Refuses sizes that the C side's int does not hold (ctypes would cut them)."""
+    if max(sizes) > 0x7fffffff:
+        raise MolgridError(MG_ESHAPE, name)
+
+
 # torch's own short way to the number of the current device
 _current_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
 
@@ -714,6 +721,7 @@ def mg_mx8_weight_gradient(grad, packed: MXTensor, natoms=None, grad_weight=None
     if natoms is not None and len(packed.shape) != 3:
         raise ValueError("natoms needs x of shape [B,N,E], got %s" % (packed.shape,))
     number, stride = _number(grad.dtype, "grad"), _row_stride(grad, "grad")
+    _fits("mg_mx8_weight_gradient", B, N, T, E)
     L = lib()
     ws, size = _workspace_of(L.mg_mx8_weight_gradient_workspace, grad, B, N, T, E)
     if grad_weight is None:
@@ -757,6 +765,7 @@ def mg_mx4_product(a: MXTensor, b: MXTensor, bias=None, dtype=torch.float32, out
         raise ValueError("rows of a have %d numbers, rows of b %d" % (K, Kb))
     dtype = out.dtype if out is not None else dtype
     number = _number(dtype, "dtype")
+    _fits("mg_mx4_product", M, N, K)
     out, stride = _product_out(out, a.shape[:-1] + (N,), dtype, a.codes, dev)
     _launch(lib().mg_mx4_product, dev, number, M, N, K, ac, asc, bc, bsc,
             _optional(bias, torch.float32, "bias", (N,), dev), out.data_ptr(), stride)
@@ -779,6 +788,7 @@ def mg_mx4_linear(x, weight: MXTensor, bias=None, out=None):
         raise ValueError("rows of x have %d numbers, rows of weight %d" % (shape[-1], K))
     number, stride = _number(x.dtype, "x"), _row_stride(x, "x")
     M = shape[0] if len(shape) == 2 else shape[:-1].numel()
+    _fits("mg_mx4_linear", M, N, K)
     out, ostride = _product_out(out, shape[:-1] + (N,), x.dtype, x, dev)
     fn = lib().mg_mx4_linear
     args = (number, M, N, K, x.data_ptr(), stride, wc, wsc, _optional(bias, torch.float32, "bias", (N,), dev),

@@ -175,3 +175,10 @@ def test_the_native_side_leaves_other_calls_alone():
     assert b.linear(x, codes, scales, (4, 40), None, 0, 0) is None
     with pytest.raises(TypeError):
         b.bind(1)
+
+
+def test_sizes_past_an_int_are_refused():
+    molgrid._fits("mg_mx4_product", 1, 0x7fffffff)
+    with pytest.raises(molgrid.MolgridError) as e:
+        molgrid._fits("mg_mx4_product", 5, 1 << 32)
+    assert e.value.code == ESHAPE
