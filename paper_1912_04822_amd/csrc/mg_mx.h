@@ -19,6 +19,7 @@ enum class Num { F32 = 0, F16 = 1, BF16 = 2 };              // the MG_F32 ... co
 enum class Mx { INT8 = 0, E4M3 = 1, E2M1 = 2 };             // the MG_MX_INT8 ... codes
 
 constexpr int kMxBlock = 32;
+constexpr int64_t kMemoryCacheBytes = 256ll << 20;      // the chip's memory-side cache
 
 __host__ __device__ inline int64_t mx_blocks(int64_t cols) { return (cols + kMxBlock - 1) / kMxBlock; }
 __host__ __device__ inline int64_t mx_scale_pitch(int64_t cols) { return (mx_blocks(cols) + 3) & ~(int64_t)3; }

@@ -22,8 +22,6 @@ __device__ inline void store16(void *p, v4u v) { __builtin_memcpy(p, &v, 16); }
 // A tensor that is larger than the memory-side cache is not found there by whoever comes next: it is read or
 // written past the caches (137 -> 119 and 131 -> 110 us for 0.62 GB of floats), aligned as it must be for that.
 // Smaller ones are not: what was just produced is still there, and what is restored is read again at once.
-constexpr int64_t kMemoryCacheBytes = 256ll << 20;
-
 bool streamed(const void *p, int64_t rows, int64_t row_stride, int64_t cols, int bytes)
 {
     return rows * cols * bytes > kMemoryCacheBytes && ((uintptr_t)p & 15) == 0 &&

@@ -262,6 +262,12 @@ __device__ inline void load_to_lds(const uint8_t *base, uint32_t offset, uint32_
     asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2\n\ts_mov_b32 m0, %0"
                  : "=&s"(m0) : "v"(offset), "s"(base), "s"(lds) : "memory");
 }
+__device__ inline void load_word_to_lds(const float *base, uint32_t offset, uint32_t lds)       // 4 bytes per lane
+{
+    uint32_t m0;
+    asm volatile("s_mov_b32 %0, m0\n\ts_mov_b32 m0, %3\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2\n\ts_mov_b32 m0, %0"
+                 : "=&s"(m0) : "v"(offset), "s"(base), "s"(lds) : "memory");
+}
 __device__ inline uint32_t lds_address(const v4u *p)
 {
     return __builtin_amdgcn_readfirstlane((uint32_t)(uintptr_t)(__attribute__((address_space(3))) const void *)p);
@@ -279,8 +285,9 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     constexpr int kTile = 64 * WT;
     constexpr int kBuffer = kTile * 16;                     // 16-byte pieces of a buffer: codes of A, then of B
     constexpr int kLoads = 4 * WT;                          // a wavefront's loads of a buffer, 8 rows each
-    __shared__ v4u lds[2 * kBuffer + 2 * kTile];            // then 16 bytes of scales for every row of A and B
-    v4u *const lds_s = lds + 2 * kBuffer;
+    // then 16 bytes of scales for every row of A and B, and the bias
+    __shared__ v4u lds[2 * kBuffer + 2 * kTile + kTile / 4];
+    v4u *const lds_s = lds + 2 * kBuffer, *const lds_bias = lds_s + 2 * kTile;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int r = lane & 31, h = lane >> 5;                 // an operand: row r, the h-th 32 of its 64 k
     const int wm = wave >> 1, wn = wave & 1;
@@ -373,6 +380,12 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     Scales scales, later;
     Operands even, odd;
     const int last_pair = (steps - 1) >> 1;
+    if (wave < WT) {
+        if (p.bias)
+            load_word_to_lds(p.bias + n0, 4 * (uint32_t)min(wave * 64 + lane, p.N - n0 - 1), lds_address(lds_bias) + wave * 256);
+        else
+            ((float *)lds_bias)[wave * 64 + lane] = 0.0f;
+    }
     fetch_scales(0);
 #pragma unroll
     for (int q = 0; q < 2; ++q) {
@@ -439,54 +452,69 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
         one(std::integral_constant<int, 3>{});
     }
 
-    // A wavefront turns its results through LDS, 32 rows of 32 WT at a time (rows 16 bytes further apart, so
-    // that 16 of them cover all banks), and stores 16 bytes per lane, rows at a stretch, past the caches where they
-    // are aligned: 4096 x 4096 x 1024 into bfloat16 takes 16.9 us so and 24.2 with ordinary stores, 31.9 and 37.0
-    // together with a kernel that reads the result.  Kept short: a small product runs through this code once, and
-    // waits for it to come from memory.
+    // A wavefront turns its results, already of their type, through LDS, 32 rows of 32 WT at a time (rows 16 bytes
+    // further apart for the banks), and stores 16 bytes per lane, rows at a stretch.  A part of C that is full goes
+    // past the caches where its rows begin with a line: 4096 x 4096 x 1024 into bfloat16 takes 17 us so and 24 with
+    // ordinary stores, 32 and 37 together with a kernel that reads the result.  Where rows share lines, only a
+    // result that the memory-side cache does not hold does: 8000 x 1004 x 500 into floats 11.5 us with ordinary
+    // stores and 14.7 past the caches, 100000 x 1000 x 1000 179 and 160.  Kept short: a small product runs through
+    // this code once, and waits for it to come from memory (2040 x 509 x 1000 7.3 us; with a choice of stores also
+    // at the edges 7.7).
     using E = typename NumTraits<T>::type;
-    constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kPitch = 32 * WT + 4;
+    constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kRows = 64 / kLanes;
+    constexpr int kPitch = 32 * WT * sizeof(E) + 16;
+    const int at_m = m0 + wm * 32 * WT, at_n = n0 + wn * 32 * WT;
+    const uintptr_t c_bits = (uintptr_t)p.c | (uintptr_t)(p.c_stride * sizeof(E));
+    const bool past = (c_bits & ((int64_t)p.M * p.N * (int)sizeof(E) > kMemoryCacheBytes ? 15 : 127)) == 0;
+    const bool inside = past && at_m + 32 * WT <= p.M && at_n + 32 * WT <= p.N;
     wait_loads<0>();
     __builtin_amdgcn_s_barrier();
-    float *const mine = (float *)(lds + wave * (kBuffer / 2));
-    const int col = P * (lane % kLanes), n = n0 + wn * 32 * WT + col;
-    const bool aligned = (((uintptr_t)p.c | (uintptr_t)(p.c_stride * sizeof(E))) & 15) == 0;
-    float bias[P];
-#pragma unroll
-    for (int e = 0; e < P; ++e) bias[e] = p.bias && n + e < p.N ? p.bias[n + e] : 0.0f;
+    uint8_t *const mine = (uint8_t *)(lds + wave * (kBuffer / 2));
+    const float *const bias = (const float *)lds_bias + wn * 32 * WT;
+    const int part = lane % kLanes, first = lane / kLanes, n = at_n + P * part;
 #pragma unroll
     for (int i = 0; i < WT; ++i) {
 #pragma unroll
-        for (int j = 0; j < WT; ++j)
+        for (int j = 0; j < WT; ++j) {
+            if constexpr (WT == 4) asm volatile("" : "+a"(acc[i][j]));  // it stays in its accumulators until here
 #pragma unroll
             for (int q = 0; q < 4; ++q) {
-                const v4f v = {acc[i][j][4 * q], acc[i][j][4 * q + 1], acc[i][j][4 * q + 2], acc[i][j][4 * q + 3]};
-                *(v4f *)(mine + r * kPitch + 32 * j + 8 * q + 4 * h) = v;
+                const int c = 32 * j + 8 * q + 4 * h;
+                const v4f b = *(const v4f *)(bias + c);
+                E e[4];
+#pragma unroll
+                for (int d = 0; d < 4; ++d) e[d] = (E)(acc[i][j][4 * q + d] + b[d]);
+                __builtin_memcpy(mine + r * kPitch + c * sizeof(E), e, sizeof(e));
             }
+        }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-#pragma unroll 2
-        for (int t = 0; t < 32 * kLanes / 64; ++t) {
-            const int row = t * (64 / kLanes) + lane / kLanes;
-            const float *from = mine + row * kPitch + col;
-            E e[P];
+        const uint8_t *const from = mine + first * kPitch + 16 * part;
+        const int m = at_m + 32 * i + first;
+        E *const to = (E *)p.c + (int64_t)m * p.c_stride + n;
+        if (inside) {
 #pragma unroll
-            for (int c = 0; c < P; c += 4) {
-                const v4f v = *(const v4f *)(from + c);
+            for (int t = 0; t < 32; t += kRows)
+                __builtin_nontemporal_store(*(const v4u *)(from + t * kPitch), (v4u *)(to + t * p.c_stride));
+        } else {
+#pragma unroll 1
+            for (int t0 = 0; t0 < 32; t0 += 4 * kRows) {
+                v4u v[4];
 #pragma unroll
-                for (int d = 0; d < 4; ++d) e[c + d] = (E)(v[d] + bias[c + d]);
-            }
-            const int m = m0 + (wm * WT + i) * 32 + row;
-            if (m >= p.M) continue;
-            E *to = (E *)p.c + (int64_t)m * p.c_stride + n;
-            if (n + P <= p.N) {
-                v4u v;
-                __builtin_memcpy(&v, e, 16);
-                if (aligned) __builtin_nontemporal_store(v, (v4u *)to);
-                else __builtin_memcpy(to, e, 16);
-            } else {
+                for (int s = 0; s < 4; ++s) v[s] = *(const v4u *)(from + (t0 + s * kRows) * kPitch);
 #pragma unroll
-                for (int d = 0; d < P; ++d)
-                    if (n + d < p.N) to[d] = e[d];
+                for (int s = 0; s < 4; ++s) {
+                    const int t = t0 + s * kRows;
+                    if (m + t >= p.M) continue;
+                    if (n + P <= p.N) {
+                        __builtin_memcpy(to + t * p.c_stride, &v[s], 16);
+                        continue;
+                    }
+                    E e[P];
+                    __builtin_memcpy(e, &v[s], 16);
+#pragma unroll
+                    for (int d = 0; d < P; ++d)
+                        if (n + d < p.N) to[t * p.c_stride + d] = e[d];
+                }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
