@@ -210,7 +210,10 @@ class AtomTyper(torch.nn.Module):
 
     What the weight gradient needs of the features is kept in 8 bits (``keep`` "int8" or "e4m3") and
     the gradient formed from the codes; ``keep=None`` leaves both to torch.  With ``natoms`` [B] (int32)
-    atoms past an example's count have no part in any gradient, whatever their rows hold."""
+    atoms past an example's count have no part in any gradient, whatever their rows hold.
+
+    A training step can be captured in a graph; as for every leaf in torch, no graph of the same
+    parameters that was recorded outside may be alive at the capture (drop losses and outputs first)."""
 
     def __init__(self, features, channels, bias=True, keep="int8", device=None, dtype=None):
         super().__init__()

@@ -523,10 +523,14 @@ def _mx_layout(shape, format):
 _BLOCK_BYTES = {"int8": 32, "e4m3": 32, "e2m1": 16}
 
 
-def _mx_pointers(t, name, formats, dev):
-    """Checks an MXTensor; (rows, columns, codes, scales)."""
+def _is_packed(t, name):
     if not isinstance(t, MXTensor):
         raise TypeError("%s must be an MXTensor, got %s" % (name, type(t).__name__))
+
+
+def _mx_pointers(t, name, formats, dev):
+    """Checks an MXTensor; (rows, columns, codes, scales)."""
+    _is_packed(t, name)
     if t.format not in formats:
         raise ValueError("%s must be in %s, got %s" % (name, " or ".join(formats), t.format))
     rows, cols, cshape, sshape = _mx_layout(t.shape, t.format)
@@ -679,8 +683,9 @@ def mg_mx_pack(x, format="int8", out: Optional[MXTensor] = None) -> MXTensor:
 
 def mg_mx_unpack(packed: MXTensor, dtype=None, out=None):
     """The numbers ``packed`` stands for, as a tensor of its shape (``dtype``: default its own)."""
+    _is_packed(packed, "packed")
     dev = _device(packed.codes, "packed.codes")
-    if out is None and isinstance(packed, MXTensor):
+    if out is None:
         native = _native(dev)
         if native is not None:
             r = native.unpack(packed.codes, packed.scales, packed.shape, MX_FORMATS.get(packed.format),
@@ -750,9 +755,10 @@ def _product_out(out, shape, dtype, like, dev):
 
 def mg_mx4_product(a: MXTensor, b: MXTensor, bias=None, dtype=torch.float32, out=None):
     """``a`` [...,K] times ``b`` [N,K] transposed, plus ``bias`` [N] (float32): [...,N] of ``dtype``."""
+    _is_packed(a, "a")
+    _is_packed(b, "b")
     dev = _device(a.codes, "a.codes")
-    if (out is None and isinstance(a, MXTensor) and isinstance(b, MXTensor) and a.format == "e2m1"
-            and b.format == "e2m1"):
+    if out is None and a.format == "e2m1" and b.format == "e2m1":
         native = _native(dev)
         if native is not None:
             r = native.product(a.codes, a.scales, a.shape, b.codes, b.scales, b.shape, bias, NUMBERS.get(dtype), dev,

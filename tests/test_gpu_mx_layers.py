@@ -349,3 +349,40 @@ def test_features_of_any_layout():
         with torch.no_grad():
             four = typer.in_4_bits()
             assert torch.equal(four(view(b)), four(copy))
+
+
+def test_a_training_step_in_a_graph():
+    """Forward and backward of features, types and grid captured once; every replay is the eager step on what
+    the features then hold.  No graph of the same leaves is alive at the capture."""
+    w, pose = grid_case(B=2, seed=13)
+    layer = GridLayer(w.resolution, w.dimension, typer=AtomTyper(40, w.T).cuda())
+    x = torch.randn((w.B, w.N, 40), device="cuda", requires_grad=True)
+    coords, radii = dev(w.coords), dev(w.radii)
+    natoms = torch.tensor([w.N, w.N // 2], dtype=torch.int32, device="cuda")
+    leaves = [x] + list(layer.parameters())
+
+    def step(G):
+        with saved_in_8_bits(min_elements=1):
+            grid = layer(coords, radii, features=x, natoms=natoms, **pose)
+        return [grid.detach()] + list(torch.autograd.grad(grid, leaves, G))
+
+    shape = layer(coords, radii, features=x, natoms=natoms, **pose).shape
+    G = torch.randn(shape, device="cuda")
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step(G)
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step(G)
+    for k in range(4):
+        with torch.no_grad():
+            x.normal_()
+            natoms.copy_(torch.tensor([w.N - k, 3 * k], dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(out, step(G)):
+            assert torch.equal(got, want), k

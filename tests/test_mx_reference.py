@@ -182,3 +182,13 @@ def test_sizes_past_an_int_are_refused():
     with pytest.raises(molgrid.MolgridError) as e:
         molgrid._fits("mg_mx4_product", 5, 1 << 32)
     assert e.value.code == ESHAPE
+
+
+def test_plain_tensors_in_place_of_packed_ones_are_refused():
+    x = torch.zeros((4, 32))
+    packed = molgrid.MXTensor(x.to(torch.uint8), x.to(torch.uint8), (4, 32), "e2m1")
+    for call in (lambda: molgrid.mg_mx_unpack(x), lambda: molgrid.mg_mx4_product(x, packed),
+                 lambda: molgrid.mg_mx4_product(packed, x), lambda: molgrid.mg_mx4_linear(x, x),
+                 lambda: molgrid.mg_mx8_weight_gradient(x, x)):
+        with pytest.raises(TypeError):
+            call()
