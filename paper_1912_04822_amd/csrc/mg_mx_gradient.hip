@@ -87,7 +87,12 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
     constexpr int kCols = 64 * Words;
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const int c = lane & 15, g = lane >> 4;
-    const int etile = blockIdx.x, ttile = blockIdx.y, split = blockIdx.z;
+    // Tiles of the same rows run on the same XCD (workgroup number modulo 8), whose L2 gives them the gradients
+    // and scales they share: 33.0 -> 28.0 us with 8 tiles, 17.5 -> 16.6 with 2 (sizes as above).
+    const int etiles = gridDim.x, ttiles = gridDim.y, total = etiles * ttiles * gridDim.z;
+    const int number = blockIdx.x + etiles * (blockIdx.y + ttiles * blockIdx.z), xcd = number % 8;
+    const int id = xcd * (total / 8) + min(xcd, total % 8) + number / 8;
+    const int etile = id % etiles, ttile = id / etiles % ttiles, split = id / (etiles * ttiles);
 
     // Columns past the end read the last valid ones and are not stored.  Lane c of an operand stands for
     // channels first .. first + Q - 1: the last lanes overlap the ones before where Q does not divide T.
