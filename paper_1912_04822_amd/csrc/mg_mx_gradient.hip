@@ -21,9 +21,9 @@
 //   - The rows are split over workgroups and the eight wavefronts of each; partial sums are added in a
 //     fixed order (LDS, then a second kernel over the workgroups' sums), so the same call gives the same
 //     bits every time.
-// Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 17.3 us (38 MB: 2.2 TB/s; the
-// first kernel 14.5, 3 to 4 steps a wavefront and their vector instructions, 5 a code); 96000 live of 128000 x
-// 1000 e4m3, 28 of bfloat16 33 us (110 MB: 3.3 TB/s); 512000 x 256 e4m3 36 us (4.5 TB/s).
+// Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 16.6 us (38 MB: 2.3 TB/s; the
+// first kernel 14, 3 to 4 steps a wavefront and their vector instructions, 5 a code); 96000 live of 128000 x
+// 1000 e4m3, 28 of bfloat16 28 us (110 MB: 3.9 TB/s); 512000 x 256 e4m3 32 us (5.1 TB/s).
 #include "mg_common.h"
 #include "mg_mx.h"
 #include "mg_mx_ops.h"

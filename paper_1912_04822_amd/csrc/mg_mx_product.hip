@@ -7,9 +7,10 @@
 //
 // The operands are given as (B, A), so a lane's four results are 4 neighbouring n of one row m of C.
 //
-// Measured: 16320 x 4096 x 4096 into bfloat16 153 us (3.6 PFLOP/s; of it 28 us for a quarter of k and about 40
-// that do not depend on k: 134 MB of results, four rounds of workgroups); 2040 x 509 x 1000 7.2; plain rows of
-// 102000 x 256 floats to 28 columns 23.4 (116 MB: 5.0 TB/s); one row by 4096 x 4096 6.0 (8.9 MB of weights).
+// Measured: 16320 x 4096 x 4096 into bfloat16 149 us (3.7 PFLOP/s; of it 29 us for a quarter of k and about 33
+// that do not depend on k: 134 MB of results, four rounds of workgroups; 185 us in a loop of nothing else);
+// 2040 x 509 x 1000 7.4; plain rows of 102000 x 256 floats to 28 columns 23.4 (116 MB: 5.0 TB/s); one row by
+// 4096 x 4096 6.0 (8.9 MB of weights).
 #include <type_traits>
 
 #include "mg_common.h"
@@ -458,7 +459,7 @@ __global__ __launch_bounds__(256, WT == 4 ? 1 : 2) void product_tile_kernel(Prod
     // ordinary stores, 32 and 37 together with a kernel that reads the result.  Where rows share lines, only a
     // result that the memory-side cache does not hold does: 8000 x 1004 x 500 into floats 11.5 us with ordinary
     // stores and 14.7 past the caches, 100000 x 1000 x 1000 179 and 160.  Kept short: a small product runs through
-    // this code once, and waits for it to come from memory (2040 x 509 x 1000 7.3 us; with a choice of stores also
+    // this code once, and waits for it to come from memory (2040 x 509 x 1000 7.4 us; with a choice of stores also
     // at the edges 7.7).
     using E = typename NumTraits<T>::type;
     constexpr int P = 16 / NumTraits<T>::bytes, kLanes = 32 * WT / P, kRows = 64 / kLanes;
