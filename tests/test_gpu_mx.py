@@ -406,3 +406,59 @@ def test_calls_on_two_streams_at_once():
         torch.cuda.synchronize()
         for k in (0, 1):
             assert all(torch.equal(a, b) for a, b in zip(got[k], want[k]))
+
+
+@pytest.mark.parametrize("K", [2112, 2200, 2400, 2530, 3100])
+def test_product_in_large_tiles(K):
+    """Enough tiles of 256 x 256 and k for them to be taken; ends of k in each of four steps, edges of C both ways.
+    Against the product in double of what the codes stand for."""
+    torch.manual_seed(K)
+    M, N = 4090, 4070
+    a, b = mgd.mg_mx_pack(torch.randn((M, K), device="cuda"), "e2m1"), mgd.mg_mx_pack(torch.randn((N, K), device="cuda"), "e2m1")
+    bias = torch.randn(N, device="cuda") if K % 100 else None
+    x, y = mgd.mg_mx_unpack(a).double(), mgd.mg_mx_unpack(b).double()
+    want, bound = x @ y.t(), K * 2.0 ** -24 * (x.abs() @ y.t().abs())
+    if bias is not None:
+        want += bias
+        bound += 2.0 ** -23 * (want.abs() + bias.abs())
+    for dtype in (torch.float32, torch.float16, torch.bfloat16):
+        half = torch.finfo(dtype).eps / 2
+        tiny = float(torch.finfo(dtype).smallest_normal) * half if dtype == torch.float16 else 0.0
+        got = mgd.mg_mx4_product(a, b, bias=bias, dtype=dtype).double()
+        assert ((got - want).abs() <= bound + half * (want.abs() + bound) + tiny).all(), dtype
+
+
+# 16 x 16, 32 x 32, 128 x 128 and 256 x 256 tiles of C, with parts that are full and edges both ways
+@pytest.mark.parametrize("size", [(40, 60, 96), (300, 700, 160), (700, 1100, 416), (4090, 4090, 2200)],
+                         ids=lambda s: "x".join(map(str, s)))
+@pytest.mark.parametrize("dtype", DTYPES)
+def test_where_results_go(size, dtype):
+    """Rows that begin with a line, with 16 bytes, anywhere: the dense call's numbers, with and without a bias,
+    and nothing written between the rows or behind the last."""
+    (M, N, K), dtype = size, DTYPES[dtype]
+    torch.manual_seed(M + N)
+    a, b = mgd.mg_mx_pack(torch.randn((M, K), device="cuda"), "e2m1"), mgd.mg_mx_pack(torch.randn((N, K), device="cuda"), "e2m1")
+    bias = torch.randn(N, device="cuda")
+    line, piece = 128 // dtype.itemsize, 16 // dtype.itemsize
+    lines = (N + line - 1) // line * line
+    for use in (None, bias):
+        want = mgd.mg_mx4_product(a, b, bias=use, dtype=dtype)
+        for pitch, start in ((lines, 0), (lines + piece, 0), (lines, piece), (lines + 1, 0), (lines, 1)):
+            room = torch.full((start + M * pitch + 64,), 7.0, dtype=dtype, device="cuda")
+            out = room[start:start + M * pitch].view(M, pitch)[:, :N]
+            mgd.mg_mx4_product(a, b, bias=use, out=out)
+            assert torch.equal(out, want), (pitch, start)
+            out.fill_(7.0)
+            assert (room == 7.0).all(), (pitch, start)
+
+
+def test_results_past_the_memory_side_cache():
+    """More than 256 MB of results, whose rows share lines: the numbers of two calls on half the rows."""
+    torch.manual_seed(3)
+    M, N, K = 70000, 1004, 100
+    a, b = mgd.mg_mx_pack(torch.randn((M, K), device="cuda"), "e2m1"), mgd.mg_mx_pack(torch.randn((N, K), device="cuda"), "e2m1")
+    got, half = mgd.mg_mx4_product(a, b), M // 2
+    assert got.numel() * 4 > 256 << 20
+    for rows in (slice(0, half), slice(half, M)):
+        part = mgd.MXTensor(a.codes[rows], a.scales[rows], (half, K), "e2m1")
+        assert torch.equal(mgd.mg_mx4_product(part, b), got[rows])
