@@ -307,7 +307,8 @@ int mg_backward_vector_f64(const mg_gridmaker *gm, int B, int N, int T,
  *     element      = x * 2^(127-S) to the nearest, ties to even, saturating
  *     value        = element * 2^(S-127)
  * A block that holds an infinity or a NaN has S = 255 and codes 0, and every
- * value of it is NaN.
+ * value of it is NaN.  Codes made elsewhere count as what they are, e4m3's 0x7f
+ * and 0xff (which mg_mx_pack does not make) as NaN.
  *     MG_MX_INT8   whole numbers -127..127       emax 6   over 255/128
  *     MG_MX_E4M3   4 significant bits, +-448     emax 8   over 29/16
  *     MG_MX_E2M1   0 .5 1 1.5 2 3 4 6 (4 bits)   emax 2   over 7/4

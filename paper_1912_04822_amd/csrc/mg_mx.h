@@ -54,6 +54,12 @@ __device__ inline float mx_inverse(uint32_t s)
     return mx_bits(s < 254u ? (254u - s) << 23 : (s == 254u ? 0x400000u : 0u));
 }
 
+// 2^(S-127), S = 0 being subnormal; NaN for S = 255
+__device__ inline float mx_power(uint32_t s)
+{
+    return mx_bits(s == 0u ? 0x400000u : s == 255u ? 0x7fc00000u : s << 23);
+}
+
 // Four elements (already divided by the scale) as one word: int8 and e4m3 a byte each.
 template <Mx F> __device__ inline uint32_t mx_encode4(const float *y)
 {

@@ -156,11 +156,12 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t *codes, 
             decode4<F>(w[u][0], f);
             if constexpr (P == 8) decode4<F>(w[u][1], f + 4);
         }
+        const float scale = mx_power((uint32_t)s[u]);       // a NaN scale or e4m3's NaN codes make a NaN
         constexpr float top = T == Num::F16 ? 65504.0f : T == Num::BF16 ? 0x1.fep127f : 0x1.fffffep127f;
 #pragma unroll
         for (int i = 0; i < P; ++i) {
-            const float v = fminf(fmaxf(ldexpf(f[i], s[u] - 127), -top), top);
-            f[i] = s[u] == 255 ? __builtin_nanf("") : v;
+            // the bounds that hand a NaN on (fminf and fmaxf would make it finite)
+            f[i] = __builtin_elementwise_minimum(__builtin_elementwise_maximum(f[i] * scale, -top), top);
         }
         const v4u out = narrow<T>(f);
         const int64_t c = (int64_t)blk[u] * kMxBlock + sub * P;
