@@ -166,7 +166,8 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
             const uint32_t w = (uint32_t)__builtin_amdgcn_ds_bpermute(scale_from + 4 * i, (int)r.scale);
-            s[i] = mx_bits(((w >> shift) & 255u) << 23);        // S = 255: infinity; times code 0, or read as a scale, NaN
+            s[i] = mx_bits(((w >> shift) & 255u) << 23);
+            if (F == Mx::INT8) s[i] = fmaf(s[i], 0.0f, s[i]);   // S = 255: infinity made NaN (e4m3: read as a scale)
         }
         if (r.live != 0xffffffffu) {
             const uint32_t mine = r.live >> (8 * g);

@@ -29,3 +29,16 @@ def test_every_e4m3_code(dtype, scale):
     assert want.isnan().sum() == 2
     for got in (mgd.mg_mx_unpack(packed, dtype=t), mgd.mg_mx_unpack(packed, out=torch.empty((8, 32), dtype=t, device="cuda"))):
         assert same(got, want)
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("T", [3, 20])
+def test_a_block_of_scale_255_is_nan_whatever_its_codes(fmt, dtype, T):
+    codes = torch.randint(1, 120, (40, 64), generator=torch.Generator().manual_seed(1)).to(torch.uint8)
+    scales = torch.full((40, 4), 120, dtype=torch.uint8)
+    scales[7, 1] = 255
+    packed = mgd.MXTensor(codes.cuda(), scales.cuda(), (40, 64), fmt)
+    assert mgd.mg_mx_unpack(packed)[7, 32:].isnan().all()
+    dw, db = mgd.mg_mx8_weight_gradient(torch.ones((40, T), device="cuda", dtype=DTYPES[dtype]), packed)
+    assert dw[:, 32:].isnan().all() and dw[:, :32].isfinite().all() and (db == 40).all()
