@@ -197,7 +197,12 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
                 gp[q][p] = __builtin_bit_cast(v8bf, w);
                 if (p + 1 < kPieces<T>) {
 #pragma unroll
-                    for (int i = 0; i < 8; ++i) rest[i] -= mx_bits(mx_word(rest[i]) & 0xffff0000u);
+                    for (int i = 0; i < 8; ++i) {
+                        // An infinity is whole in its first piece.  Looking for it costs 15.3 -> 15.7 us at 102000 x
+                        // 256 x 28; no less behind a test of all, or by rows walked again where the sums are NaN.
+                        const float more = rest[i] - mx_bits(mx_word(rest[i]) & 0xffff0000u);
+                        rest[i] = p == 0 && __builtin_isinf(rest[i]) ? 0.0f : more;
+                    }
                 }
             }
         }

@@ -42,3 +42,39 @@ def test_a_block_of_scale_255_is_nan_whatever_its_codes(fmt, dtype, T):
     assert mgd.mg_mx_unpack(packed)[7, 32:].isnan().all()
     dw, db = mgd.mg_mx8_weight_gradient(torch.ones((40, T), device="cuda", dtype=DTYPES[dtype]), packed)
     assert dw[:, 32:].isnan().all() and dw[:, :32].isfinite().all() and (db == 40).all()
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("fmt", ["int8", "e4m3"])
+@pytest.mark.parametrize("T,E", [(3, 20), (5, 100), (20, 100)])
+def test_infinite_gradients(fmt, dtype, T, E):
+    """An infinity in the gradient is one in the sums it belongs to: of its sign times the number's, NaN where the
+    number is 0, where both signs meet or where a NaN stands beside it."""
+    t, inf = DTYPES[dtype], float("inf")
+    gen = torch.Generator().manual_seed(T)
+    x = torch.randn((1, 70, E), generator=gen)
+    x[0, 5, 4] = 0.0
+    x[0, 5, 6] = x[0, 9, 6]
+    x[0, 5, 7], x[0, 9, 7] = x[0, 9, 7].abs(), -x[0, 9, 7].abs()
+    g = torch.randn((1, 70, T), generator=gen).to(t)
+    g[0, 5, 0], g[0, 9, 1], g[0, 5, 2], g[0, 9, 2] = inf, -inf, inf, -inf
+    if T > 3:
+        g[0, 69, 3], g[0, 5, 4], g[0, 33, 4] = torch.finfo(t).max / 4, inf, float("nan")
+    packed = mgd.mg_mx_pack(x.cuda(), fmt)
+    xv = mgd.mg_mx_unpack(packed).double().cpu()[0]
+    want = (g[0].double().t()[:, None, :] * xv.t()[None]).sum(2)
+    dw, db = (v.double().cpu() for v in mgd.mg_mx8_weight_gradient(g.cuda(), packed))
+    odd = ~want.isfinite()
+    assert odd[:3].all() and want[0].isinf().any() and want[2].isnan().any()
+    assert same(dw[odd], want[odd])
+    bound = 3 * 70 * 2.0 ** -24 * (g[0].double().t().abs() @ xv.abs())     # three pieces, three sums
+    assert ((dw - want).abs()[~odd] <= bound[~odd]).all()
+    assert same(db[:3], torch.tensor([inf, -inf, float("nan")]))
+
+
+def test_gradient_bits_that_only_the_low_half_of_a_float_holds():
+    """A NaN of low payload bits alone stays one."""
+    g = torch.ones((1, 40, 3))
+    g.view(torch.int32)[0, 3, 1] = 0x7f800001
+    dw, db = mgd.mg_mx8_weight_gradient(g.cuda(), mgd.mg_mx_pack(torch.ones((1, 40, 33), device="cuda")))
+    assert dw[1].isnan().all() and db[1].isnan() and (dw[[0, 2]] == 40).all() and (db[[0, 2]] == 40).all()
