@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
         uint32_t b = (__umulhi(m0, a.div_mul) + m0) >> a.div_shift, from = m0 - b * a.N, live = 0;
         for (uint32_t done = 0; done < rows; ++b, from = 0) {
             const uint32_t run = min(a.N - from, rows - done);      // of example b
-            const int left = min(max(a.natoms[b] - (int)from, 0), (int)run);
+            const int left = min(max(max(a.natoms[b], 0) - (int)from, 0), (int)run);
             if (left > 0) live |= (0xffffffffu >> (kRows - left)) << done;
             done += run;
         }

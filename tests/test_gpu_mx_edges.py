@@ -78,3 +78,17 @@ def test_gradient_bits_that_only_the_low_half_of_a_float_holds():
     g.view(torch.int32)[0, 3, 1] = 0x7f800001
     dw, db = mgd.mg_mx8_weight_gradient(g.cuda(), mgd.mg_mx_pack(torch.ones((1, 40, 33), device="cuda")))
     assert dw[1].isnan().all() and db[1].isnan() and (dw[[0, 2]] == 40).all() and (db[[0, 2]] == 40).all()
+
+
+@pytest.mark.parametrize("N", [1, 31, 100, 1000])
+def test_counts_at_the_ends_of_their_type(N):
+    """Counts below 0 are 0 and counts above N are N, also where steps of rows start inside an example."""
+    low, high = -1 << 31, (1 << 31) - 1
+    x = mgd.mg_mx_pack(torch.randn((5, N, 70), device="cuda", generator=torch.Generator("cuda").manual_seed(N)))
+    g = torch.randn((5, N, 6), device="cuda", generator=torch.Generator("cuda").manual_seed(N + 1))
+    count = lambda *n: torch.tensor(n, dtype=torch.int32, device="cuda")
+    got = mgd.mg_mx8_weight_gradient(g, x, natoms=count(low, high, low + 5, N // 2, high - 1))
+    want = mgd.mg_mx8_weight_gradient(g, x, natoms=count(0, N, 0, N // 2, N))
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    for out in mgd.mg_mx8_weight_gradient(g, x, natoms=count(*[low] * 5)):
+        assert not out.any()
