@@ -169,9 +169,9 @@ class _TypeWeights(torch.autograd.Function):
         weight, natoms, codes, scales = ctx.saved_tensors
         gx = gw = gb = None
         grad = grad.contiguous()
-        if natoms is not None and (ctx.needs_input_grad[0] or not ctx.needs_input_grad[1]):
-            grad = _live_rows(grad, natoms)
         if ctx.needs_input_grad[0]:
+            if natoms is not None:
+                grad = _live_rows(grad, natoms)
             gx = torch.matmul(grad.view(-1, grad.shape[2]), weight.float()).view(ctx.shape).to(ctx.dtypes[0])
         if ctx.needs_input_grad[1]:
             packed = molgrid.MXTensor(codes, scales, ctx.shape, ctx.keep)
@@ -181,7 +181,7 @@ class _TypeWeights(torch.autograd.Function):
             gb = None
         else:
             if gb is None:                          # a bias alone
-                gb = grad.view(-1, grad.shape[2]).sum(0)
+                gb = _sum_of_rows(grad, natoms)
             gb = gb.to(ctx.dtypes[2])
         return gx, gw, gb, None, None
 
@@ -201,6 +201,14 @@ def _live_rows(x, natoms):
     """``x`` [B,N,...] with zeros past every example's ``natoms``."""
     live = torch.arange(x.shape[1], device=x.device)[None, :] < natoms[:, None]
     return torch.where(live[:, :, None], x, torch.zeros((), dtype=x.dtype, device=x.device))
+
+
+def _sum_of_rows(grad, natoms):
+    """Sum of the live rows of ``grad`` [B,N,T]: the bias that goes with weights of one feature, whose codes are
+    zeros.  (torch's sum over many rows gives wrong numbers when a graph it was captured in is replayed.)"""
+    B, N, _ = grad.shape
+    codes, scales = (torch.zeros((B * N, k), dtype=torch.uint8, device=grad.device) for k in (32, 4))
+    return molgrid.mg_mx8_weight_gradient(grad, molgrid.MXTensor(codes, scales, (B, N, 1), "int8"), natoms=natoms)[1]
 
 
 class AtomTyper(torch.nn.Module):

@@ -1,0 +1,66 @@
+"""Learned types and tensors saved in 8 bits where they are used in ways of their own: parts of them frozen, in
+graphs at full size, under autocast, with batches that are empty."""
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+from paper_1912_04822_amd.autograd import AtomTyper  # noqa: E402
+
+
+def captured(step):
+    """``step`` in a graph, after three runs on a stream of its own; the graph and what the step returns."""
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for _ in range(3):
+            step()
+    torch.cuda.current_stream().wait_stream(side)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = step()
+    return graph, out
+
+
+@pytest.mark.parametrize("trained", ["weight and bias", "weight", "bias", "features"])
+def test_a_step_of_a_whole_batch_in_a_graph(trained):
+    """102000 atoms: every replay gives the eager step's numbers, whatever part of the layer learns."""
+    torch.manual_seed(1)
+    typer = AtomTyper(64, 28).cuda()
+    x = torch.randn((50, 2040, 64), device="cuda")
+    leaves = {"weight and bias": [typer.weight, typer.bias], "weight": [typer.weight], "bias": [typer.bias], "features": [x]}[trained]
+    for v in (typer.weight, typer.bias, x):
+        v.requires_grad_(any(v is leaf for leaf in leaves))
+    G = torch.randn((50, 2040, 28), device="cuda")
+    natoms = torch.full((50,), 2040, dtype=torch.int32, device="cuda")
+
+    def step():
+        return torch.autograd.grad(typer(x, natoms), leaves, G)
+
+    graph, out = captured(step)
+    for k in range(4):
+        G.normal_()
+        natoms.copy_(torch.randint(0, 2041, (50,), dtype=torch.int32))
+        graph.replay()
+        torch.cuda.synchronize()
+        for got, want in zip(out, step()):
+            assert torch.equal(got, want), k
+
+
+@pytest.mark.parametrize("ragged", [False, True])
+def test_a_bias_that_learns_alone(ragged):
+    torch.manual_seed(2)
+    B, N, T = 7, 333, 5
+    typer = AtomTyper(33, T).cuda()
+    typer.weight.requires_grad_(False)
+    x, G = torch.randn((B, N, 33), device="cuda"), torch.randn((B, N, T), device="cuda")
+    natoms, live = None, torch.ones((B, N), dtype=torch.bool, device="cuda")
+    if ragged:
+        natoms = torch.tensor([333, 0, 1, 32, 33, -4, 1000], dtype=torch.int32, device="cuda")
+        live = torch.arange(N, device="cuda")[None] < natoms[:, None]
+        G[~live] = float("nan")
+    typer(x, natoms).backward(G)
+    g = G.double()[live]
+    bound = len(g) * 2.0 ** -24 * g.abs().sum(0)            # a float sum in any order
+    assert typer.weight.grad is None and ((typer.bias.grad.double() - g.sum(0)).abs() <= bound).all()
