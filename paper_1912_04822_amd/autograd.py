@@ -186,6 +186,49 @@ class _TypeWeights(torch.autograd.Function):
         return gx, gw, gb, None, None
 
 
+class _LiveMap(torch.autograd.Function):
+    """A linear map of [B,N,E] whose gradients leave out the rows past ``natoms``, whatever features and gradients
+    hold there, from torch's operations alone."""
+
+    generate_vmap_rule = True
+
+    @staticmethod
+    def forward(features, weight, bias, natoms):
+        return torch.nn.functional.linear(features, weight, bias)
+
+    @staticmethod
+    def setup_context(ctx, inputs, output):
+        ctx.save_for_backward(*inputs)
+        ctx.save_for_forward(*inputs)
+
+    @staticmethod
+    def backward(ctx, grad):
+        features, weight, bias, natoms = ctx.saved_tensors
+        gx = gw = gb = None
+        grad = _live_rows(grad, natoms)
+        flat = grad.flatten(0, 1)
+        if ctx.needs_input_grad[0]:
+            gx = torch.matmul(grad, weight.to(grad.dtype)).to(features.dtype)
+        if ctx.needs_input_grad[1]:
+            live = _live_rows(features, natoms).flatten(0, 1)
+            gw = torch.matmul(flat.t(), live.to(grad.dtype)).to(weight.dtype)
+        if bias is not None and ctx.needs_input_grad[2]:
+            gb = flat.sum(0).to(bias.dtype)
+        return gx, gw, gb, None
+
+    @staticmethod
+    def jvp(ctx, features_t, weight_t, bias_t, _):
+        features, weight, bias, natoms = ctx.saved_tensors
+        y = torch.zeros((), dtype=features.dtype, device=features.device)
+        if features_t is not None:
+            y = y + torch.nn.functional.linear(_live_rows(features_t, natoms), weight)
+        if weight_t is not None:
+            y = y + torch.nn.functional.linear(_live_rows(features, natoms), weight_t)
+        if bias_t is not None:
+            y = y + bias_t
+        return _live_rows(y.expand(*features.shape[:2], weight.shape[0]), natoms)
+
+
 def _even_rows(x):
     """``x``, or a copy where its rows are not equally far apart (expanded, transposed)."""
     return x if molgrid.row_stride(x) is not None else x.contiguous()
@@ -242,10 +285,10 @@ class AtomTyper(torch.nn.Module):
             raise ValueError("features must have shape [B,N,%d], got %s"
                              % (self.weight.shape[1], tuple(features.shape)))
         _check_natoms(natoms, features)
-        if self.keep is None or not torch.is_grad_enabled():
-            if natoms is not None and torch.is_grad_enabled():
-                features = _live_rows(features, natoms)
+        if not torch.is_grad_enabled() or (self.keep is None and natoms is None):
             return torch.nn.functional.linear(features, self.weight, self.bias).float()
+        if self.keep is None:
+            return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
         with _Exact():
             return _TypeWeights.apply(features, self.weight, self.bias, natoms, self.keep)
 

@@ -1,0 +1,62 @@
+"""Learned types and tensors saved in 8 bits, the parts that run without a device."""
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_1912_04822_amd.autograd import AtomTyper, _LiveMap  # noqa: E402
+
+
+@pytest.mark.parametrize("bias", [False, True])
+def test_plain_typer_leaves_out_what_lies_past_the_counts(bias):
+    """With ``keep=None``: the live rows' gradients, also where the others' features and gradients are NaN, and the
+    same forward values with gradients and without."""
+    torch.manual_seed(1)
+    B, N, E, T = 4, 6, 5, 3
+    typer = AtomTyper(E, T, bias=bias, keep=None)
+    natoms = torch.tensor([6, 2, 0, 1], dtype=torch.int32)
+    live = torch.arange(N)[None] < natoms[:, None]
+    x, G = torch.randn((B, N, E)), torch.randn((B, N, T))
+    for dead in (1.0, float("nan")):
+        x[~live], G[~live] = dead, dead
+        leaf = x.clone().requires_grad_()
+        typer.zero_grad()
+        y = typer(leaf, natoms)
+        y.backward(G)
+        with torch.no_grad():
+            assert torch.equal(torch.nan_to_num(y, 7.0), torch.nan_to_num(typer(x, natoms), 7.0))
+        g, xs = G[live].double(), x[live].double()
+        eps = 2.0 ** -24 * live.sum()
+        assert ((typer.weight.grad - g.t() @ xs).abs() <= eps * (g.abs().t() @ xs.abs())).all()
+        if bias:
+            assert ((typer.bias.grad - g.sum(0)).abs() <= eps * g.abs().sum(0)).all()
+        w = typer.weight.detach().double()
+        assert (leaf.grad[~live] == 0).all()
+        assert ((leaf.grad[live] - g @ w).abs() <= T * 2.0 ** -24 * (g.abs() @ w.abs())).all()
+
+
+def test_plain_typer_is_differentiated_like_any_map():
+    """Gradients and their gradients against differences, forward mode, and over a batch of parameters."""
+    torch.manual_seed(2)
+    x, w, b = (torch.randn(s, dtype=torch.float64, requires_grad=True) for s in ((3, 4, 5), (2, 5), (2,)))
+    natoms = torch.tensor([4, 0, 2], dtype=torch.int32)
+    live = (torch.arange(4)[None] < natoms[:, None])[:, :, None]
+    only_live = lambda x, w, b: torch.where(live, _LiveMap.apply(x, w, b, natoms), 0.0)     # rows past it have no gradient
+    assert torch.autograd.gradcheck(only_live, (x, w, b), check_forward_ad=True)
+    assert torch.autograd.gradgradcheck(only_live, (x, w, b))
+    assert torch.autograd.gradcheck(lambda x, w: torch.where(live, _LiveMap.apply(x, w, None, natoms), 0.0), (x, w))
+    ws = torch.randn((6, 2, 5), dtype=torch.float64)
+    got = torch.func.vmap(lambda v: torch.func.grad(lambda u: _LiveMap.apply(x.detach(), u, b.detach(), natoms).sum())(v))(ws)
+    assert torch.allclose(got, torch.where(live, x.detach(), 0.0).sum((0, 1)).expand(6, 2, 5))
+
+
+def test_plain_typer_under_autocast():
+    torch.manual_seed(3)
+    typer = AtomTyper(8, 4, keep=None)
+    x = torch.randn((2, 5, 8), requires_grad=True)
+    natoms = torch.tensor([5, 2], dtype=torch.int32)
+    with torch.autocast("cpu", dtype=torch.bfloat16):
+        y = typer(x, natoms)
+    assert y.dtype == torch.float32
+    y.sum().backward()
+    assert x.grad.dtype == typer.weight.grad.dtype == typer.bias.grad.dtype == torch.float32
+    assert (typer.bias.grad == 7).all() and (x.grad[1, 2:] == 0).all()
