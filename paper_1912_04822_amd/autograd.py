@@ -285,11 +285,11 @@ class AtomTyper(torch.nn.Module):
             raise ValueError("features must have shape [B,N,%d], got %s"
                              % (self.weight.shape[1], tuple(features.shape)))
         _check_natoms(natoms, features)
-        if not torch.is_grad_enabled() or (self.keep is None and natoms is None):
-            return torch.nn.functional.linear(features, self.weight, self.bias).float()
-        if self.keep is None:
-            return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
         with _Exact():
+            if not torch.is_grad_enabled() or (self.keep is None and natoms is None):
+                return torch.nn.functional.linear(features, self.weight, self.bias).float()
+            if self.keep is None:
+                return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
             return _TypeWeights.apply(features, self.weight, self.bias, natoms, self.keep)
 
     def in_4_bits(self):

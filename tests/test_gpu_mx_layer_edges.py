@@ -5,7 +5,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from paper_1912_04822_amd.autograd import AtomTyper  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, saved_in_8_bits  # noqa: E402
 
 
 def captured(step):
@@ -64,3 +64,18 @@ def test_a_bias_that_learns_alone(ragged):
     g = G.double()[live]
     bound = len(g) * 2.0 ** -24 * g.abs().sum(0)            # a float sum in any order
     assert typer.weight.grad is None and ((typer.bias.grad.double() - g.sum(0)).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("counts", [False, True])
+def test_what_a_plain_typer_saves_stays_exact(counts):
+    """``keep=None`` within ``saved_in_8_bits``: the gradients it has outside."""
+    torch.manual_seed(3)
+    typer = AtomTyper(100, 6, keep=None).cuda()
+    x, G = torch.randn((2, 400, 100), device="cuda", requires_grad=True), torch.randn((2, 400, 6), device="cuda")
+    natoms = torch.tensor([400, 30], dtype=torch.int32, device="cuda") if counts else None
+    leaves = [x, typer.weight, typer.bias]
+    want = torch.autograd.grad(typer(x * 1.0, natoms), leaves, G)
+    with saved_in_8_bits(min_elements=1):
+        y = typer(x * 1.0, natoms)
+    for got, w in zip(torch.autograd.grad(y, leaves, G), want):
+        assert torch.equal(got, w)
