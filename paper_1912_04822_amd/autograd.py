@@ -107,8 +107,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         loss.backward()
 
     Kept so: float32, float16 and bfloat16 device tensors of at least ``min_elements`` numbers that
-    lie without gaps in memory, but for parameters (leaves that require a gradient) and views of them,
-    which exist anyway.  Everything else, and what this module's own layers save, stays exact.  ``format``
+    lie without gaps in memory, but for parameters (frozen ones too), other leaves that require a
+    gradient, and views of either, which exist anyway.  Everything else, and what this module's own layers save, stays exact.  ``format``
     "int8" is off by at most 2^-7 of the block's largest number, "e4m3" by at most 2^-4 of each.
     Gradients change accordingly; small positive numbers of a block may become zero (and with them
     the gradient of a ReLU there), and a block that holds an infinity or a NaN becomes NaN."""
@@ -141,7 +141,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
 
 def _is_parameter(x):
-    return x.is_leaf and x.requires_grad
+    return isinstance(x, torch.nn.Parameter) or (x.is_leaf and x.requires_grad)
 
 
 def _in_memory_order(x):

@@ -1,5 +1,7 @@
 """Learned types and tensors saved in 8 bits where they are used in ways of their own: parts of them frozen, in
 graphs at full size, under autocast, with batches that are empty."""
+import contextlib
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -79,3 +81,34 @@ def test_what_a_plain_typer_saves_stays_exact(counts):
         y = typer(x * 1.0, natoms)
     for got, w in zip(torch.autograd.grad(y, leaves, G), want):
         assert torch.equal(got, w)
+
+
+LAYERS = {"linear": (lambda: torch.nn.Linear(100, 90), (3, 70, 100)),
+          "flat linear": (lambda: torch.nn.Linear(100, 90), (70, 100)),
+          "convolution": (lambda: torch.nn.Conv3d(8, 8, 3, padding=1), (2, 8, 9, 9, 9))}
+
+
+def input_gradients(layer, shape, context):
+    """What reaches the input, which hangs on the weights alone."""
+    torch.manual_seed(4)
+    x = torch.randn(shape, device="cuda", requires_grad=True)
+    with context:
+        y = layer(x * 1.0)
+    return torch.autograd.grad(y, x, torch.ones_like(y))[0]
+
+
+def rounding(layer):
+    """How far two float sums of the weights that meet in a number of the input's gradient can lie apart: each is
+    off by at most n 2^-24 of their magnitudes.  Weights in 8 bits are off by up to 2^-8 of the largest."""
+    w = layer.weight.detach().transpose(0, 1).flatten(1)
+    return 2 * w.shape[1] * 2.0 ** -24 * w.abs().sum(1).max()
+
+
+@pytest.mark.parametrize("layer", LAYERS)
+@pytest.mark.parametrize("frozen", [False, True])
+def test_weights_stay_exact(layer, frozen):
+    make, shape = LAYERS[layer]
+    layer = make().cuda().requires_grad_(not frozen)
+    want = input_gradients(layer, shape, contextlib.nullcontext())
+    got = input_gradients(layer, shape, saved_in_8_bits(min_elements=1))
+    assert ((got - want).abs() <= rounding(layer)).all()

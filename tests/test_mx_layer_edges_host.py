@@ -3,7 +3,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from paper_1912_04822_amd.autograd import AtomTyper, _LiveMap  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, _LiveMap, _is_parameter  # noqa: E402
 
 
 @pytest.mark.parametrize("bias", [False, True])
@@ -60,3 +60,27 @@ def test_plain_typer_under_autocast():
     y.sum().backward()
     assert x.grad.dtype == typer.weight.grad.dtype == typer.bias.grad.dtype == torch.float32
     assert (typer.bias.grad == 7).all() and (x.grad[1, 2:] == 0).all()
+
+
+def taken_for_parameters(run):
+    """What autograd saves while ``run`` runs: (shape, whether it counts as a parameter or a view of one)."""
+    seen = []
+
+    def look(x):
+        seen.append((tuple(x.shape), _is_parameter(x) or (x._base is not None and _is_parameter(x._base))))
+        return x
+
+    with torch.autograd.graph.saved_tensors_hooks(look, lambda x: x):
+        run()
+    return seen
+
+
+@pytest.mark.parametrize("frozen", [False, True])
+def test_weights_are_told_from_activations(frozen):
+    x = torch.randn((7, 9), requires_grad=True) * 1.0
+    linear = torch.nn.Linear(9, 5).requires_grad_(not frozen)
+    seen = dict(taken_for_parameters(lambda: linear(x)))
+    assert seen[(9, 5) if (9, 5) in seen else (5, 9)] and not seen.get((7, 9), False)
+    x = torch.randn((2, 3, 6, 6), requires_grad=True) * 1.0
+    seen = dict(taken_for_parameters(lambda: torch.nn.Conv2d(3, 4, 3).requires_grad_(not frozen)(x)))
+    assert seen[(4, 3, 3, 3)] and not seen[(2, 3, 6, 6)]
