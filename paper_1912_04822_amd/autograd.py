@@ -108,7 +108,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     Kept so: float32, float16 and bfloat16 device tensors of at least ``min_elements`` numbers that
     lie without gaps in memory, but for parameters (frozen ones too), other leaves that require a
-    gradient, and views of either, which exist anyway.  Everything else, and what this module's own layers save, stays exact.  ``format``
+    gradient, and views of either, which exist anyway, and the copies autocast makes of them in another type.
+    (Its copies of frozen weights cannot be told from data: have a frozen layer in the type it runs in.)  Everything else, and what this module's own layers save, stays exact.  ``format``
     "int8" is off by at most 2^-7 of the block's largest number, "e4m3" by at most 2^-4 of each.
     Gradients change accordingly; small positive numbers of a block may become zero (and with them
     the gradient of a ReLU there), and a block that holds an infinity or a NaN becomes NaN."""
@@ -141,7 +142,11 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
 
 def _is_parameter(x):
-    return isinstance(x, torch.nn.Parameter) or (x.is_leaf and x.requires_grad)
+    if isinstance(x, torch.nn.Parameter) or (x.is_leaf and x.requires_grad):
+        return True
+    if x.grad_fn is None or x.grad_fn.name() != "ToCopyBackward0":
+        return False
+    return hasattr(x.grad_fn.next_functions[0][0], "variable")     # a copy of a leaf in another type
 
 
 def _in_memory_order(x):

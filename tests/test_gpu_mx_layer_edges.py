@@ -112,3 +112,25 @@ def test_weights_stay_exact(layer, frozen):
     want = input_gradients(layer, shape, contextlib.nullcontext())
     got = input_gradients(layer, shape, saved_in_8_bits(min_elements=1))
     assert ((got - want).abs() <= rounding(layer)).all()
+
+
+@pytest.mark.parametrize("layer", LAYERS)
+def test_weights_stay_exact_under_autocast(layer):
+    """The copies of the weights in bfloat16 are saved as they are, the input in 8 bits."""
+    make, shape = LAYERS[layer]
+    layer = make().cuda()
+    seen = []
+
+    class Look(saved_in_8_bits):
+        def _pack(self, x):
+            kept = super()._pack(x)
+            seen.append((x.numel(), isinstance(kept, torch.Tensor)))
+            return kept
+
+    x = torch.randn(shape, device="cuda", requires_grad=True)
+    with Look(min_elements=1), torch.autocast("cuda", dtype=torch.bfloat16):
+        y = layer(x * 1.0)
+    n = layer.weight.numel()
+    assert (n, True) in seen and (n, False) not in seen and (x.numel(), False) in seen
+    y.float().sum().backward()
+    assert x.grad.isfinite().all() and layer.weight.grad.dtype == torch.float32

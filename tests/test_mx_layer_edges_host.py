@@ -84,3 +84,17 @@ def test_weights_are_told_from_activations(frozen):
     x = torch.randn((2, 3, 6, 6), requires_grad=True) * 1.0
     seen = dict(taken_for_parameters(lambda: torch.nn.Conv2d(3, 4, 3).requires_grad_(not frozen)(x)))
     assert seen[(4, 3, 3, 3)] and not seen[(2, 3, 6, 6)]
+
+
+def test_copies_of_weights_are_told_from_activations():
+    x = torch.randn((7, 9), requires_grad=True) * 1.0
+    image = torch.randn((2, 3, 6, 6), requires_grad=True) * 1.0
+    linear, conv = torch.nn.Linear(9, 5), torch.nn.Conv2d(3, 4, 3)
+    with torch.autocast("cpu", dtype=torch.bfloat16):
+        seen = dict(taken_for_parameters(lambda: linear(x)))
+        assert seen[(9, 5) if (9, 5) in seen else (5, 9)] and not seen.get((7, 9), False)
+        seen = dict(taken_for_parameters(lambda: conv(image)))
+        assert seen[(4, 3, 3, 3)] and not seen[(2, 3, 6, 6)]
+    twice = (x * x).to(torch.bfloat16)                  # copies of activations are activations
+    seen = dict(taken_for_parameters(lambda: twice * twice))
+    assert not seen[(7, 9)]
