@@ -9,6 +9,7 @@ from __future__ import annotations
 import ctypes
 import importlib.util
 import os
+import warnings
 from typing import Optional
 
 import torch
@@ -37,6 +38,7 @@ BINDING_PATH = os.path.join(_HERE, "_binding.so")
 
 _lib: Optional[ctypes.CDLL] = None
 _binding = None         # the C++ side of the microscaled-format calls, loaded with the library
+_no_binding = None      # why it was not, until the first such call has said so
 
 
 class MolgridError(RuntimeError):
@@ -49,7 +51,7 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
     """Load libmolgrid_hip.so (built by ``paper_1912_04822_amd.build``); raise if absent.
     ``path`` (first call only) names another build of the same library, e.g. the measurement
     build with the timing aids."""
-    global _lib
+    global _lib, _no_binding
     if _lib is None:
         path = path or LIB_PATH
         if not os.path.exists(path):
@@ -122,13 +124,17 @@ def lib(path: Optional[str] = None) -> ctypes.CDLL:
         L.mg_set_option.argtypes = [ctypes.c_char_p, ci]
         L.mg_time_next_kernel.restype = ci
         L.mg_time_next_kernel.argtypes = [vp, vp]
-        _load_binding(L)
         _lib = L
+        try:
+            _load_binding(L)
+        except (ImportError, OSError) as e:
+            _no_binding = str(e)
     return _lib
 
 
 def _load_binding(L) -> None:
-    """Load the C++ side of the binding and hand it the addresses of the library's functions."""
+    """Load the C++ side of the binding and hand it the addresses of the library's functions.  It is built against
+    one version of torch; without it every call goes through ctypes to the same kernels."""
     global _binding
     if not os.path.exists(BINDING_PATH):
         raise FileNotFoundError(
@@ -629,10 +635,14 @@ def _launch(fn, dev, *args):
 def _native(dev):
     """The C++ side of the binding, which takes calls on the current device in their common form (dense
     tensors, new results) and returns None for any other, or None."""
+    global _no_binding
     if dev < 0 or _raw_stream is None or dev != _current_device():
         return None
     if _binding is None:
         lib()
+        if _no_binding is not None:
+            why, _no_binding = _no_binding, None
+            warnings.warn("calls on microscaled formats take 4 us more host time each: " + why)
     return _binding
 
 

@@ -92,3 +92,21 @@ def test_counts_at_the_ends_of_their_type(N):
     assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
     for out in mgd.mg_mx8_weight_gradient(g, x, natoms=count(*[low] * 5)):
         assert not out.any()
+
+
+def test_calls_without_the_binding(monkeypatch):
+    """Where the C++ side is missing the same kernels give the same bits."""
+    x = torch.randn((3, 50, 70), device="cuda")
+    w = torch.randn((30, 70), device="cuda")
+    g = torch.randn((3, 50, 6), device="cuda")
+
+    def work():
+        packed, four = mgd.mg_mx_pack(x), mgd.mg_mx_pack(w, "e2m1")
+        return (packed.codes, packed.scales, mgd.mg_mx_unpack(packed), *mgd.mg_mx8_weight_gradient(g, packed),
+                mgd.mg_mx4_linear(x, four), mgd.mg_mx4_product(mgd.mg_mx_pack(x, "e2m1"), four))
+
+    want = work()
+    assert mgd._binding is not None
+    monkeypatch.setattr(mgd, "_binding", None)
+    for a, b in zip(work(), want):
+        assert torch.equal(a, b)

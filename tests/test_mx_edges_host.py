@@ -1,0 +1,28 @@
+"""Calls on microscaled formats as far as they go without a device."""
+import warnings
+
+import pytest
+
+torch = pytest.importorskip("torch")
+
+from paper_1912_04822_amd import molgrid  # noqa: E402
+
+
+@pytest.mark.parametrize("found", [None, b"not a library"])
+def test_the_library_does_without_the_binding(found, tmp_path, monkeypatch):
+    """Grids need only the library; what is missing or does not load is said once, by the first call it slows down."""
+    path = tmp_path / "_binding.so"
+    if found is not None:
+        path.write_bytes(found)
+    for name, value in (("_lib", None), ("_binding", None), ("_no_binding", None), ("BINDING_PATH", str(path)),
+                        ("_raw_stream", lambda dev: 0), ("_current_device", lambda: 0)):
+        monkeypatch.setattr(molgrid, name, value)
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        gm = molgrid.GridMaker(0.5, 23.5)
+        assert gm.D == 48 and molgrid._native(-1) is None
+    with pytest.warns(UserWarning, match="_binding.so"):
+        assert molgrid._native(0) is None
+    with warnings.catch_warnings():
+        warnings.simplefilter("error")
+        assert molgrid._native(0) is None
