@@ -291,7 +291,7 @@ class AtomTyper(torch.nn.Module):
                              % (self.weight.shape[1], tuple(features.shape)))
         _check_natoms(natoms, features)
         with _Exact():
-            if not torch.is_grad_enabled() or (self.keep is None and natoms is None):
+            if not torch.is_grad_enabled() or (self.keep is None and natoms is None) or features.numel() == 0:
                 return torch.nn.functional.linear(features, self.weight, self.bias).float()
             if self.keep is None:
                 return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
@@ -321,6 +321,8 @@ class AtomTyper4(torch.nn.Module):
             raise RuntimeError("a typer in 4 bits has no gradient")
         if features.dim() != 3 or features.shape[2] != self.features:
             raise ValueError("features must have shape [B,N,%d], got %s" % (self.features, tuple(features.shape)))
+        if features.numel() == 0:
+            return features.new_empty(features.shape[:2] + (self.codes.shape[0],), dtype=torch.float32)
         weight = molgrid.MXTensor(self.codes, self.scales, (self.codes.shape[0], self.features), "e2m1")
         bias = None if self.bias is None else self.bias.float()
         return molgrid.mg_mx4_linear(_even_rows(features), weight, bias).float()

@@ -134,3 +134,18 @@ def test_weights_stay_exact_under_autocast(layer):
     assert (n, True) in seen and (n, False) not in seen and (x.numel(), False) in seen
     y.float().sum().backward()
     assert x.grad.isfinite().all() and layer.weight.grad.dtype == torch.float32
+
+
+@pytest.mark.parametrize("size", [(0, 5), (3, 0), (0, 0)])
+@pytest.mark.parametrize("keep", [None, "int8", "e4m3"])
+def test_batches_without_atoms(keep, size):
+    typer = AtomTyper(8, 4, keep=keep).cuda()
+    x = torch.zeros(size + (8,), device="cuda", requires_grad=True)
+    for natoms in (None, torch.zeros(size[0], dtype=torch.int32, device="cuda")):
+        typer.zero_grad()
+        y = typer(x, natoms)
+        assert y.shape == size + (4,) and y.dtype == torch.float32
+        y.sum().backward()
+        assert not typer.weight.grad.any() and not typer.bias.grad.any() and x.grad.shape == x.shape
+    y = typer.in_4_bits()(x.detach())
+    assert y.shape == size + (4,) and y.dtype == torch.float32 and y.is_cuda
