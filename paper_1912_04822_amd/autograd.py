@@ -243,6 +243,8 @@ def _check_natoms(natoms, features):
     if natoms is not None and (natoms.dtype is not torch.int32 or tuple(natoms.shape) != (features.shape[0],)):
         raise ValueError("natoms must be int32 of shape (%d,), got %s of %s"
                          % (features.shape[0], natoms.dtype, tuple(natoms.shape)))
+    if natoms is not None and natoms.device != features.device and torch.is_grad_enabled():
+        raise ValueError("natoms is on %s, features are on %s" % (natoms.device, features.device))
 
 
 def _live_rows(x, natoms):
@@ -295,6 +297,7 @@ class AtomTyper(torch.nn.Module):
                 return torch.nn.functional.linear(features, self.weight, self.bias).float()
             if self.keep is None:
                 return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
+            natoms = None if natoms is None else natoms.contiguous()
             return _TypeWeights.apply(features, self.weight, self.bias, natoms, self.keep)
 
     def in_4_bits(self):

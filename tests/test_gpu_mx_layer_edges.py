@@ -149,3 +149,17 @@ def test_batches_without_atoms(keep, size):
         assert not typer.weight.grad.any() and not typer.bias.grad.any() and x.grad.shape == x.shape
     y = typer.in_4_bits()(x.detach())
     assert y.shape == size + (4,) and y.dtype == torch.float32 and y.is_cuda
+
+
+@pytest.mark.parametrize("keep", [None, "int8"])
+def test_counts_of_any_stride(keep):
+    """What the backward pass needs of the counts is taken or refused at the call."""
+    torch.manual_seed(5)
+    typer = AtomTyper(8, 4, keep=keep).cuda()
+    x = torch.randn((3, 40, 8), device="cuda")
+    table = torch.tensor([[40, 1], [7, 2], [0, 3]], dtype=torch.int32, device="cuda")
+    want = torch.autograd.grad(typer(x, table[:, 0].contiguous()).sum(), [typer.weight, typer.bias])
+    for got, w in zip(torch.autograd.grad(typer(x, table[:, 0]).sum(), [typer.weight, typer.bias]), want):
+        assert torch.equal(got, w)
+    with pytest.raises(ValueError):
+        typer(x, table[:, 0].cpu())
