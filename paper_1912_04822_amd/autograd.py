@@ -271,7 +271,8 @@ class AtomTyper(torch.nn.Module):
     atoms past an example's count have no part in any gradient, whatever their rows hold.
 
     A training step can be captured in a graph; as for every leaf in torch, no graph of the same
-    parameters that was recorded outside may be alive at the capture (drop losses and outputs first)."""
+    parameters that was recorded outside may be alive at the capture (drop losses and outputs first).
+    With ``keep=None`` the bias's gradient is torch's sum, which over many atoms is wrong when replayed."""
 
     def __init__(self, features, channels, bias=True, keep="int8", device=None, dtype=None):
         super().__init__()
