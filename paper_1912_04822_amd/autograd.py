@@ -99,8 +99,11 @@ class _Exact:
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Within ``with saved_in_8_bits():`` what autograd saves for the backward pass is kept in 8 bits
     (blocks of 32 neighbouring numbers in memory that share a power of two) and restored when it is
-    needed: a quarter of the memory of float32 activations, half of 16-bit ones.  For the network
-    behind a grid, whose activations are as large as the grid:
+    needed.  Every save takes 33/32 bytes a number.  What several operations save (a ReLU's result is the next
+    convolution's input) is kept once for each of them, where torch holds it once: four convolutions
+    followed by ReLU take 0.41 of their float32 memory and 0.83 of bfloat16's, by softplus, where
+    nothing is saved twice, 0.26 and 0.52.  For the network behind a grid, whose activations are as
+    large as the grid:
 
         with saved_in_8_bits():
             loss = net(layer(coords, radii, types=types, T=T))

@@ -163,3 +163,33 @@ def test_counts_of_any_stride(keep):
         assert torch.equal(got, w)
     with pytest.raises(ValueError):
         typer(x, table[:, 0].cpu())
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+@pytest.mark.parametrize("act,tensors,saves", [(torch.nn.ReLU, 5, 8), (torch.nn.Softplus, 8, 8)], ids=["relu", "softplus"])
+def test_what_a_network_saves_takes_the_bytes_it_is_said_to(act, tensors, saves, dtype):
+    """Four convolutions and as many activations: torch holds the input and every result that an operation saves
+    once (softplus saves its input, so nothing twice), 8 bits hold 33/32 bytes a number for every save."""
+    net = torch.nn.Sequential(*[m for _ in range(4) for m in (torch.nn.Conv3d(16, 16, 3, padding=1), act())]).cuda().to(dtype)
+    x = torch.randn((4, 16, 32, 32, 32), device="cuda", dtype=dtype)
+    plain, kept = {}, []
+
+    def hold(t):
+        if not isinstance(t, torch.nn.Parameter):
+            plain[t.untyped_storage().data_ptr()] = t       # held, so no address comes twice
+        return t
+
+    class Count(saved_in_8_bits):
+        def _pack(self, t):
+            k = super()._pack(t)
+            if isinstance(k, tuple):
+                kept.append(k[0].codes.nbytes + k[0].scales.nbytes)
+            return k
+
+    with torch.autograd.graph.saved_tensors_hooks(hold, lambda t: t):
+        net(x * 1.0)
+    with Count():
+        net(x * 1.0)
+    n = x.numel()
+    assert sum(t.numel() for t in plain.values() if t.numel() == n) == tensors * n
+    assert kept == [n + n // 32] * saves
