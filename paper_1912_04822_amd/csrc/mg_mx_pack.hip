@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void pack_kernel(const unsigned char *x, 
 {
     constexpr int P = kPerLane<T>, L = kMxBlock / P;
     constexpr uint32_t kBlocks = kThreads / L;              // blocks a workgroup takes at a time
-    const uint32_t first = blockIdx.x * (kBlocks * Unroll) + threadIdx.x / L;
+    const uint32_t first = (blockIdx.x + blockIdx.y * gridDim.x) * (kBlocks * Unroll) + threadIdx.x / L;
     const int sub = threadIdx.x % L;
     v4u raw[Unroll];
     uint32_t at[Unroll], blk[Unroll];
@@ -114,7 +114,7 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t *codes, 
 {
     constexpr int P = kPerLane<T>, L = kMxBlock / P;
     constexpr uint32_t kBlocks = kThreads / L;
-    const uint32_t first = blockIdx.x * (kBlocks * Unroll) + threadIdx.x / L;
+    const uint32_t first = (blockIdx.x + blockIdx.y * gridDim.x) * (kBlocks * Unroll) + threadIdx.x / L;
     const int sub = threadIdx.x % L;
     uint32_t w[Unroll][2], row[Unroll], blk[Unroll];
     int s[Unroll];
@@ -182,6 +182,10 @@ __global__ __launch_bounds__(kThreads) void unpack_kernel(const uint8_t *codes, 
 
 constexpr int kUnroll = 4;
 
+// A launch counts the threads along x in 32 bits: 2^24 workgroups, which floats in 2^31 - 127 blocks or more take,
+// are one too many.
+dim3 grid(uint32_t groups) { return groups < (1u << 24) ? dim3(groups) : dim3((groups + 1) / 2, 2); }
+
 template <Num T, Mx F>
 hipError_t pack_typed(int64_t rows, int64_t cols, const void *x, int64_t row_stride, uint8_t *codes,
                       uint8_t *scales, hipStream_t stream)
@@ -191,7 +195,7 @@ hipError_t pack_typed(int64_t rows, int64_t cols, const void *x, int64_t row_str
     constexpr uint32_t per = kThreads / (kMxBlock / kPerLane<T>) * kUnroll;
     const auto kernel = streamed(x, rows, row_stride, cols, NumTraits<T>::bytes) ? pack_kernel<T, F, kUnroll, true>
                                                                                 : pack_kernel<T, F, kUnroll, false>;
-    hipLaunchKernelGGL(kernel, dim3((total + per - 1) / per), dim3(kThreads), 0, stream, (const unsigned char *)x,
+    hipLaunchKernelGGL(kernel, grid((total + per - 1) / per), dim3(kThreads), 0, stream, (const unsigned char *)x,
                        row_stride, cols, blocks, pitch, total, codes, scales);
     return hipGetLastError();
 }
@@ -205,7 +209,7 @@ hipError_t unpack_typed(int64_t rows, int64_t cols, const uint8_t *codes, const 
     constexpr uint32_t per = kThreads / (kMxBlock / kPerLane<T>) * kUnroll;
     const auto kernel = streamed(x, rows, row_stride, cols, NumTraits<T>::bytes) ? unpack_kernel<T, F, kUnroll, true>
                                                                                 : unpack_kernel<T, F, kUnroll, false>;
-    hipLaunchKernelGGL(kernel, dim3((total + per - 1) / per), dim3(kThreads), 0, stream, codes, scales, cols, blocks,
+    hipLaunchKernelGGL(kernel, grid((total + per - 1) / per), dim3(kThreads), 0, stream, codes, scales, cols, blocks,
                        pitch, total, (unsigned char *)x, row_stride);
     return hipGetLastError();
 }

@@ -110,3 +110,21 @@ def test_calls_without_the_binding(monkeypatch):
     monkeypatch.setattr(mgd, "_binding", None)
     for a, b in zip(work(), want):
         assert torch.equal(a, b)
+
+
+def test_as_many_rows_as_the_scales_allow():
+    """2^31 - 4 bytes of scales: floats of one column, whose lanes past the last row are counted past 2^32."""
+    rows = (1 << 29) - 1
+    x = torch.arange(rows, dtype=torch.int32, device="cuda").remainder_(251).sub_(120).float().view(rows, 1)
+    got = mgd.mg_mx_pack(x, "int8")
+    for k in (0, 12345678, rows - 4096):
+        want = mgd.mg_mx_pack(x[k:k + 4096].clone(), "int8")
+        assert torch.equal(got.codes[k:k + 4096], want.codes) and torch.equal(got.scales[k:k + 4096], want.scales)
+    del x
+    back = mgd.mg_mx_unpack(got)
+    bad = 0
+    for k in range(0, rows, 1 << 26):       # up to 127 numbers come back as they were; from 128 on in steps of
+        want = torch.arange(k, min(rows, k + (1 << 26)), dtype=torch.int32, device="cuda").remainder_(251).sub_(120)
+        want[want == 129] = 128             # two, 129 lies halfway and goes to 128 (64 is even)
+        bad += int((back[k:k + (1 << 26), 0] != want.float()).sum())
+    assert bad == 0
