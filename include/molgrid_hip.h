@@ -347,10 +347,11 @@ int mg_mx_unpack(int format, int dtype, int64_t rows, int64_t cols, const uint8_
  * grad: B*N rows of T numbers, grad_stride >= T elements apart; grad_weight
  * [T][E] and grad_bias [T] (may be NULL) float, written.  natoms [B] or NULL
  * (all N; a count below 0 is taken as 0, above N as N): rows past it count for
- * nothing, whatever they hold.  Codes and
- * gradients enter exactly (blocks of magnitudes below 2^-120 as zero),
- * infinities and NaN as what they are; sums are float in a fixed order.  B*N < 2^31-255, T <= 65535, E <= 2^20,
- * grad_stride <= 2^26 (else MG_ESHAPE).  The workspace (32-byte aligned) is scratch.
+ * nothing, whatever they hold.  Codes and gradients enter exactly, infinities and
+ * NaN as what they are, but for what of a number lies below 2^-133 and int8
+ * blocks of magnitudes below 2^-120, which count as zero; sums are float in a
+ * fixed order.  B*N < 2^31-255, T <= 65535, E <= 2^20, grad_stride <= 2^26 (else
+ * MG_ESHAPE).  The workspace (32-byte aligned) is scratch.
  */
 int mg_mx8_weight_gradient_workspace(int B, int N, int T, int E, size_t *bytes);
 int mg_mx8_weight_gradient(int format, int dtype, int B, int N, int T, int E, const void *grad,

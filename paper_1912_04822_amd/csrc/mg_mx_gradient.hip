@@ -15,7 +15,7 @@
 //   - A code times its power of two is exact in bfloat16 (at most 8 significant bits); int8 blocks whose
 //     scale byte is 0 (magnitudes below 2^-120) count as zero.  A float gradient is cut into three
 //     bfloat16 pieces (8 + 8 + 8 bits, exact), a half one into two, so that the products are exact and
-//     only their sum, in float, rounds.
+//     only their sum, in float, rounds.  bfloat16 ends at 2^-133: what of a number lies below it is lost.
 //   - Rows that are not live (past natoms[b], or past the end) are zeroed in both operands by a mask of
 //     the 32 rows, so that whatever they hold counts for nothing.
 //   - The rows are split over workgroups and the eight wavefronts of each; partial sums are added in a

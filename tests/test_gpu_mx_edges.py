@@ -128,3 +128,32 @@ def test_as_many_rows_as_the_scales_allow():
         want[want == 129] = 128             # two, 129 lies halfway and goes to 128 (64 is even)
         bad += int((back[k:k + (1 << 26), 0] != want.float()).sum())
     assert bad == 0
+
+
+@pytest.mark.parametrize("exponent", [-100, -110, -118, -124, -130, -140])
+def test_gradients_near_the_end_of_the_range(exponent):
+    """Float gradients with 24 significant bits: what lies above 2^-133 counts, also below the normal range."""
+    gen = torch.Generator().manual_seed(7)
+    g = (torch.randn((1, 64, 20), generator=gen, dtype=torch.float64) * 2.0 ** exponent).float()
+    x = torch.randint(-127, 128, (1, 64, 40), generator=gen).float() * 2.0 ** 60
+    packed = mgd.mg_mx_pack(x.cuda())
+    xv = mgd.mg_mx_unpack(packed).double().cpu()[0]
+    gv = g.double()[0]
+    dw, db = (v.double().cpu() for v in mgd.mg_mx8_weight_gradient(g.cuda(), packed))
+    # three sums of 64 exact products, and less than 2^-133 of every gradient
+    bound = 3 * 64 * 2.0 ** -24 * (gv.abs().t() @ xv.abs()) + 2.0 ** -133 * xv.abs().sum(0)
+    assert ((dw - gv.t() @ xv).abs() <= bound).all()
+    assert ((db - gv.sum(0)).abs() <= 64 * 2.0 ** -24 * gv.abs().sum(0) + 2.0 ** -149).all()
+
+
+def test_codes_near_the_end_of_the_range():
+    """e4m3 blocks of the lowest scales: every code above 2^-133 counts."""
+    codes = torch.arange(256, dtype=torch.uint8).view(8, 32)[[0, 1, 2, 4, 5, 6]].contiguous()
+    for scale in (0, 1, 2, 9):
+        scales = torch.full((6, 4), scale, dtype=torch.uint8)
+        packed = mgd.MXTensor(codes.cuda(), scales.cuda(), (6, 32), "e4m3")
+        xv = codes.view(torch.float8_e4m3fn).double() * 2.0 ** (scale - 127)
+        dw, _ = mgd.mg_mx8_weight_gradient(torch.full((6, 2), 2.0 ** 60, device="cuda"), packed)
+        want = xv.sum(0) * 2.0 ** 60
+        bound = 6 * 2.0 ** -24 * xv.abs().sum(0) * 2.0 ** 60 + 6 * 2.0 ** (60 - 133)
+        assert ((dw.double().cpu() - want).abs() <= bound).all()
