@@ -127,7 +127,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     def _pack(self, x):
         if (getattr(_exact, "on", False) or not x.is_cuda or x.dtype not in molgrid.NUMBERS
-                or x.numel() < self.min_elements or x.layout is not torch.strided
+                or x.numel() < self.min_elements or x.layout is not torch.strided or x.is_neg()
                 or _is_parameter(x) or (x._base is not None and _is_parameter(x._base))):
             return x
         flat = _in_memory_order(x.detach())
@@ -239,6 +239,7 @@ class _LiveMap(torch.autograd.Function):
 
 def _even_rows(x):
     """``x``, or a copy where its rows are not equally far apart (expanded, transposed)."""
+    x = x.resolve_neg()
     return x if molgrid.row_stride(x) is not None else x.contiguous()
 
 

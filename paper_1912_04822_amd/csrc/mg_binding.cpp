@@ -53,7 +53,7 @@ int64_t integer(PyObject *o)
 const at::Tensor &dense(PyObject *o, int64_t dev)
 {
     const at::Tensor &t = tensor(o);
-    plain(t.is_cuda() && t.get_device() == dev && t.layout() == at::kStrided && t.is_contiguous());
+    plain(t.is_cuda() && t.get_device() == dev && t.layout() == at::kStrided && t.is_contiguous() && !t.is_neg());
     return t;
 }
 

@@ -605,6 +605,8 @@ def row_stride(t):
 
 
 def _row_stride(t, name):
+    if t.is_neg():                              # its memory holds the numbers with the other sign
+        raise ValueError("%s is a view that negates: give %s.resolve_neg()" % (name, name))
     step = row_stride(t)
     if step is None:
         raise ValueError("the rows of %s must be contiguous and equally far apart" % name)

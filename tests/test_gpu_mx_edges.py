@@ -6,6 +6,7 @@ torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
 from paper_1912_04822_amd import molgrid as mgd  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, saved_in_8_bits  # noqa: E402
 
 DTYPES = {"float32": torch.float32, "float16": torch.float16, "bfloat16": torch.bfloat16}
 
@@ -157,3 +158,24 @@ def test_codes_near_the_end_of_the_range():
         want = xv.sum(0) * 2.0 ** 60
         bound = 6 * 2.0 ** -24 * xv.abs().sum(0) * 2.0 ** 60 + 6 * 2.0 ** (60 - 133)
         assert ((dw.double().cpu() - want).abs() <= bound).all()
+
+
+def test_views_that_negate():
+    for rows in (1, 4):
+        x = torch.full((1, rows, 1), 1.0 + 2.0j, device="cuda").conj().imag
+        w = mgd.mg_mx_pack(torch.ones((3, 1), device="cuda"), "e2m1")
+        packed = mgd.mg_mx_pack(torch.ones((1, rows, 5), device="cuda"))
+        for call in (lambda: mgd.mg_mx_pack(x), lambda: mgd.mg_mx4_linear(x, w),
+                     lambda: mgd.mg_mx8_weight_gradient(x, packed), lambda: mgd.mg_mx_unpack(mgd.mg_mx_pack(x.clone()), out=x)):
+            with pytest.raises(ValueError, match="resolve_neg"):
+                call()
+        assert (mgd.mg_mx4_linear(x.resolve_neg(), w) == -2).all()
+        typer = AtomTyper(1, 3).cuda()
+        assert torch.equal(typer.in_4_bits()(x), typer.in_4_bits()(x.resolve_neg()))
+        typer(x).sum().backward()
+        assert (typer.weight.grad == -2 * rows).all()
+    x = torch.full((1,), 1.0 + 2.0j, device="cuda", requires_grad=True)
+    with saved_in_8_bits(min_elements=1):
+        y = x.conj().imag.square()
+    y.backward()
+    assert x.grad == 4.0j                               # d (imag x)^2

@@ -26,3 +26,11 @@ def test_the_library_does_without_the_binding(found, tmp_path, monkeypatch):
     with warnings.catch_warnings():
         warnings.simplefilter("error")
         assert molgrid._native(0) is None
+
+
+def test_views_that_negate_are_refused():
+    """The imaginary part of a conjugate is a view of numbers that have the other sign in memory."""
+    x = torch.ones((4, 1), dtype=torch.complex64).conj().imag
+    assert x.is_neg() and molgrid.row_stride(x) == 2
+    with pytest.raises(ValueError, match="resolve_neg"):
+        molgrid.mg_mx_pack(x)
