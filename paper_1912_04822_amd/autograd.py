@@ -302,6 +302,10 @@ class AtomTyper(torch.nn.Module):
                 return torch.nn.functional.linear(features, self.weight, self.bias).float()
             if self.keep is None:
                 return _LiveMap.apply(features, self.weight, self.bias, natoms).float()
+            T, E = self.weight.shape
+            if (T > 65535 or E > 1 << 20) and any(p.requires_grad for p in self.parameters()):
+                raise ValueError("the gradient from 8 bits takes up to 2^20 features and 65535 channels, got %d and %d:"
+                                 " use keep=None" % (E, T))
             natoms = None if natoms is None else natoms.contiguous()
             return _TypeWeights.apply(features, self.weight, self.bias, natoms, self.keep)
 

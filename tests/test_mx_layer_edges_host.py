@@ -98,3 +98,13 @@ def test_copies_of_weights_are_told_from_activations():
     twice = (x * x).to(torch.bfloat16)                  # copies of activations are activations
     seen = dict(taken_for_parameters(lambda: twice * twice))
     assert not seen[(7, 9)]
+
+
+@pytest.mark.parametrize("E,T", [(1, 65536), ((1 << 20) + 1, 1)])
+def test_sizes_the_backward_pass_has_no_gradient_for_are_refused_at_the_call(E, T):
+    typer = AtomTyper(E, T)
+    with pytest.raises(ValueError, match="keep=None"):
+        typer(torch.zeros((1, 2, E)))
+    assert AtomTyper(E, T, keep=None)(torch.zeros((1, 2, E))).shape == (1, 2, T)
+    with torch.no_grad():
+        assert typer(torch.zeros((1, 2, E))).shape == (1, 2, T)
