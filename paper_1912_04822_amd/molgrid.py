@@ -482,6 +482,9 @@ class GridMaker:
 
 
 # ---- microscaled formats: numbers in 8 or 4 bits ----
+#
+# Like the GridMaker's, these calls record nothing for autograd: what they return has no history, also where
+# their arguments require gradients (AtomTyper and saved_in_8_bits are what differentiates).
 
 MX_FORMATS = {"int8": 0, "e4m3": 1, "e2m1": 2}          # MG_MX_INT8, MG_MX_E4M3, MG_MX_E2M1
 NUMBERS = {torch.float32: 0, torch.float16: 1, torch.bfloat16: 2}     # MG_F32, MG_F16, MG_BF16

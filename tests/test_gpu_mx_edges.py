@@ -179,3 +179,47 @@ def test_views_that_negate():
         y = x.conj().imag.square()
     y.backward()
     assert x.grad == 4.0j                               # d (imag x)^2
+
+
+@pytest.mark.parametrize("K", [6100, 6220, 6400, 6505])
+def test_product_where_large_tiles_win_by_a_tenth(K):
+    """4090 x 4070 in tiles of 256 x 256, well past the k from which they are the faster ones; ends of k in each of
+    four steps, edges of C both ways.  Against the product in double of what the codes stand for."""
+    torch.manual_seed(K)
+    M, N = 4090, 4070
+    a, b = (mgd.mg_mx_pack(torch.randn((rows, K), device="cuda"), "e2m1") for rows in (M, N))
+    bias = torch.randn(N, device="cuda")
+    x, y = mgd.mg_mx_unpack(a).double(), mgd.mg_mx_unpack(b).double().t().contiguous()
+    want, bound = x @ y, K * 2.0 ** -24 * (x.abs() @ y.abs())
+    for use in (None, bias):
+        if use is not None:
+            want, bound = want + bias, bound + 2.0 ** -23 * (want.abs() + bias.abs())
+        for dtype in DTYPES.values():
+            half = torch.finfo(dtype).eps / 2
+            tiny = float(torch.finfo(dtype).smallest_normal) * half if dtype == torch.float16 else 0.0
+            got = mgd.mg_mx4_product(a, b, bias=use, dtype=dtype).double()
+            assert ((got - want).abs() <= bound + half * (want.abs() + bound) + tiny).all(), dtype
+
+
+def test_every_block_of_a_row_longer_than_the_offsets_of_32_bits():
+    """2.1e9 half numbers whose blocks differ in size: each is off by at most half a step of its own block (at most
+    2^-7 of 256/255 of its largest: a largest number from 255/128 of a power of two on takes the next one), and by
+    half a step of its type."""
+    n = (1 << 31) + 12345
+    x = torch.empty((1, n), dtype=torch.float16, device="cuda").normal_()
+    for part in x[0, :n // 32 * 32].view(-1, 32).split(1 << 20):
+        part *= torch.randint(0, 6, (part.shape[0], 1), device="cuda").float().mul_(2).exp2_().div_(256.0)
+    back = mgd.mg_mx_unpack(mgd.mg_mx_pack(x, "int8"))
+    bad = 0
+    for a, b in zip(x[0, :n // 32 * 32].view(-1, 32).split(1 << 22), back[0, :n // 32 * 32].view(-1, 32).split(1 << 22)):
+        a, b = a.float(), b.float()
+        off = a.abs().amax(1, keepdim=True) * (2.0 ** -7 * 256 / 255) + b.abs() * 2.0 ** -11 + 2.0 ** -25
+        bad += int(((a - b).abs() > off).sum())
+    assert bad == 0
+
+
+def test_calls_on_tensors_record_no_history():
+    x = torch.randn((4, 40), device="cuda", requires_grad=True)
+    packed, w = mgd.mg_mx_pack(x), mgd.mg_mx_pack(x, "e2m1")
+    for y in (packed.codes, mgd.mg_mx_unpack(packed), mgd.mg_mx4_linear(x, w), *mgd.mg_mx8_weight_gradient(x, packed)):
+        assert not y.requires_grad
