@@ -111,11 +111,15 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
 
     Kept so: float32, float16 and bfloat16 device tensors of at least ``min_elements`` numbers that
     lie without gaps in memory, but for parameters (frozen ones too), other leaves that require a
-    gradient, and views of either, which exist anyway, and the copies autocast makes of them in another type.
-    (Its copies of frozen weights cannot be told from data: have a frozen layer in the type it runs in.)  Everything else, and what this module's own layers save, stays exact.  ``format``
-    "int8" is off by at most 2^-7 of the block's largest number, "e4m3" by at most 2^-4 of each.
-    Gradients change accordingly; small positive numbers of a block may become zero (and with them
-    the gradient of a ReLU there), and a block that holds an infinity or a NaN becomes NaN."""
+    gradient, and views of either, which exist anyway, and the copies autocast makes of them in
+    another type.  (Its copies of frozen weights cannot be told from data: have a frozen layer in the
+    type it runs in.)  Everything else, and what this module's own layers save, stays exact.
+
+    ``format`` "int8" is off by at most 2^-7 of the block's largest number (256/255 of that where the
+    largest is just below a power of two), "e4m3" by at most 2^-4 of each (or 1.2 times 2^-18 of the
+    largest, where that is more).  Gradients change accordingly; small positive numbers of a block may
+    become zero (and with them the gradient of a ReLU there), and a block that holds an infinity or a
+    NaN becomes NaN."""
 
     def __init__(self, format="int8", min_elements=1 << 16):
         if format not in ("int8", "e4m3"):
