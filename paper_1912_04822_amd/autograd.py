@@ -58,6 +58,8 @@ class _IndexGrid(torch.autograd.Function):
 class _VectorGrid(torch.autograd.Function):
     @staticmethod
     def forward(ctx, coords, weights, gm, radii, natoms, centers, quats, translations):
+        if weights.dim() != 3 or weights.shape[:2] != coords.shape[:2]:     # tables of other atoms than the weights'
+            raise ValueError("weights must have shape [%d,%d,T], got %s" % (*coords.shape[:2], tuple(weights.shape)))
         ctx.gm, ctx.ws = gm, None
         ctx.save_for_backward(coords, weights, radii, natoms, centers, quats, translations)
         if (ctx.needs_input_grad[0] or ctx.needs_input_grad[1]) and not gm.binary:

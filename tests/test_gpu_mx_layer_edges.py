@@ -7,7 +7,7 @@ import pytest
 torch = pytest.importorskip("torch")
 pytestmark = pytest.mark.gpu
 
-from paper_1912_04822_amd.autograd import AtomTyper, saved_in_8_bits  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, GridLayer, saved_in_8_bits  # noqa: E402
 
 
 def captured(step):
@@ -193,3 +193,14 @@ def test_what_a_network_saves_takes_the_bytes_it_is_said_to(act, tensors, saves,
     n = x.numel()
     assert sum(t.numel() for t in plain.values() if t.numel() == n) == tensors * n
     assert kept == [n + n // 32] * saves
+
+
+def test_features_of_other_atoms_than_the_coordinates_are_refused():
+    layer = GridLayer(0.5, 5.5, typer=AtomTyper(8, 3).cuda())
+    coords, radii = torch.zeros((2, 40, 3), device="cuda", requires_grad=True), torch.ones(3, device="cuda")
+    for shape in ((2, 20, 8), (2, 80, 8), (1, 40, 8), (4, 40, 8)):
+        with pytest.raises(ValueError, match="weights must have shape"):
+            layer(coords, radii, features=torch.zeros(shape, device="cuda"))
+        with torch.no_grad(), pytest.raises(ValueError):
+            layer(coords, radii, features=torch.zeros(shape, device="cuda"))
+    assert layer(coords, radii, features=torch.zeros((2, 40, 8), device="cuda")).shape == (2, 3, 12, 12, 12)

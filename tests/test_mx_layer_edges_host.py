@@ -3,7 +3,7 @@ import pytest
 
 torch = pytest.importorskip("torch")
 
-from paper_1912_04822_amd.autograd import AtomTyper, _LiveMap, _is_parameter  # noqa: E402
+from paper_1912_04822_amd.autograd import AtomTyper, GridLayer, _LiveMap, _is_parameter  # noqa: E402
 
 
 @pytest.mark.parametrize("bias", [False, True])
@@ -108,3 +108,17 @@ def test_sizes_the_backward_pass_has_no_gradient_for_are_refused_at_the_call(E, 
     assert AtomTyper(E, T, keep=None)(torch.zeros((1, 2, E))).shape == (1, 2, T)
     with torch.no_grad():
         assert typer(torch.zeros((1, 2, E))).shape == (1, 2, T)
+
+
+@pytest.mark.parametrize("shape", [(2, 4, 3), (2, 6, 3), (1, 5, 3), (3, 5, 3), (2, 5)])
+@pytest.mark.parametrize("learned", [False, True])
+def test_weights_of_other_atoms_than_the_coordinates_are_refused(shape, learned):
+    """Before anything reaches the device: with gradients, tables are built for the coordinates' atoms."""
+    coords, radii = torch.zeros((2, 5, 3), requires_grad=True), torch.ones(3)
+    layer = GridLayer(typer=AtomTyper(8, 3, keep=None))
+    if learned and len(shape) == 3:
+        given = dict(features=torch.zeros(shape[:2] + (8,)))
+    else:
+        given = dict(weights=torch.zeros(shape))
+    with pytest.raises(ValueError, match="weights must have shape"):
+        layer(coords, radii, **given)
