@@ -115,7 +115,7 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     lie without gaps in memory, but for parameters (frozen ones too), other leaves that require a
     gradient, and views of either, which exist anyway, and the copies autocast makes of them in
     another type.  (Its copies of frozen weights cannot be told from data: have a frozen layer in the
-    type it runs in.)  Everything else, and what this module's own layers save, stays exact.
+    type it runs in.)  Everything else, nested tensors and subclasses of tensors among it, and what this module's own layers save, stays exact.
 
     ``format`` "int8" is off by at most 2^-7 of the block's largest number (256/255 of that where the
     largest is just below a power of two), "e4m3" by at most 2^-4 of each (or 1.2 times 2^-18 of the
@@ -132,7 +132,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
         super().__init__(self._pack, self._unpack)
 
     def _pack(self, x):
-        if (getattr(_exact, "on", False) or not x.is_cuda or x.dtype not in molgrid.NUMBERS
+        if (getattr(_exact, "on", False) or type(x) is not torch.Tensor or x.is_nested or not x.is_cuda
+                or x.dtype not in molgrid.NUMBERS
                 or x.numel() < self.min_elements or x.layout is not torch.strided or x.is_neg()
                 or _is_parameter(x) or (x._base is not None and _is_parameter(x._base))):
             return x

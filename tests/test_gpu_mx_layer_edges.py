@@ -204,3 +204,21 @@ def test_features_of_other_atoms_than_the_coordinates_are_refused():
         with torch.no_grad(), pytest.raises(ValueError):
             layer(coords, radii, features=torch.zeros(shape, device="cuda"))
     assert layer(coords, radii, features=torch.zeros((2, 40, 8), device="cuda")).shape == (2, 3, 12, 12, 12)
+
+
+def test_nested_tensors_and_subclasses_are_saved_as_they_are():
+    class Named(torch.Tensor):
+        pass
+
+    torch.manual_seed(6)
+    parts = [torch.randn((n, 40), device="cuda") for n in (30, 50)]
+    nested = lambda: torch.nested.nested_tensor(parts, requires_grad=True)
+    named = lambda: parts[0].clone().as_subclass(Named).requires_grad_()
+    for make in (nested, named):
+        x = make()
+        with saved_in_8_bits(min_elements=1):
+            h = x * 1.0
+            y = h * h
+        (y.to_padded_tensor(0.0) if x.is_nested else y).sum().backward()
+        got, want = (x.grad.to_padded_tensor(0.0), x.detach().to_padded_tensor(0.0)) if x.is_nested else (x.grad, x.detach())
+        assert torch.equal(got, 2 * want)
