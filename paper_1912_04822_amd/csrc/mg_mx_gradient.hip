@@ -24,6 +24,8 @@
 // Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 16.6 us (38 MB: 2.3 TB/s; the
 // first kernel 14, 3 to 4 steps a wavefront and their vector instructions, 5 a code); 96000 live of 128000 x
 // 1000 e4m3, 28 of bfloat16 28 us (110 MB: 3.9 TB/s); 512000 x 256 e4m3 32 us (5.1 TB/s).
+#include <type_traits>
+
 #include "mg_common.h"
 #include "mg_mx.h"
 #include "mg_mx_ops.h"
@@ -160,7 +162,7 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
 #pragma unroll
     for (int q = 0; q < Q; ++q) bias[q] = 0.0f;
 
-    auto compute = [&](Step<T, Q, Words> &r) {
+    auto compute = [&](Step<T, Q, Words> &r, auto careful) {
         if (r.live == 0) return;
         float s[8];
 #pragma unroll
@@ -198,10 +200,8 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
                 if (p + 1 < kPieces<T>) {
 #pragma unroll
                     for (int i = 0; i < 8; ++i) {
-                        // An infinity is whole in its first piece.  Looking for it costs 15.3 -> 15.7 us at 102000 x
-                        // 256 x 28; no less behind a test of all, or by rows walked again where the sums are NaN.
                         const float more = rest[i] - mx_bits(mx_word(rest[i]) & 0xffff0000u);
-                        rest[i] = p == 0 && __builtin_isinf(rest[i]) ? 0.0f : more;
+                        rest[i] = careful && __builtin_isinf(rest[i]) ? 0.0f : more;
                     }
                 }
             }
@@ -256,11 +256,38 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
                 if (step >= s1) goto done;
                 ahead = mask(step + kDepth * kWaves);
                 load(step + (kDepth - 1) * kWaves, live, ring[(d + kDepth - 1) % kDepth]);
-                compute(ring[d]);
+                compute(ring[d], std::false_type{});
             }
         }
     }
 done:
+
+    // An infinity in a gradient of several pieces leaves NaN in the pieces after its first and makes its channel's
+    // sums NaN in every column.  A wavefront that finds one walks its rows once more, and there an infinity is whole in its
+    // first piece.  (Looked for in the walk above: 15.3 -> 15.7 us at 102000 x 256 x 28, 22.6 -> 23.6 at 32640 x 512 x 100.)
+    if constexpr (kPieces<T> > 1) {
+        float any = 0.0f;
+#pragma unroll
+        for (int q = 0; q < Q; ++q)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) any = __builtin_elementwise_maximum(any, acc[q][0][0][i]);
+        if (__builtin_amdgcn_ballot_w64(__builtin_isnan(any)) != 0) {
+#pragma unroll
+            for (int q = 0; q < Q; ++q) {
+                bias[q] = 0.0f;
+#pragma unroll
+                for (int w = 0; w < Words; ++w)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) acc[q][w][j] = v4f{0.0f, 0.0f, 0.0f, 0.0f};
+            }
+#pragma unroll 1
+            for (uint32_t step = s0 + wave; step < s1; step += kWaves) {
+                Step<T, Q, Words> r;
+                load(step, mask(step), r);
+                compute(r, std::true_type{});
+            }
+        }
+    }
 
     // The wavefronts' sums, 16 of a lane's channels at a time, through LDS as [wavefront][item][lane] of 4
     // columns, an item being one of a lane's four accumulator rows and one of its words; the wavefronts share

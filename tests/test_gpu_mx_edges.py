@@ -223,3 +223,26 @@ def test_calls_on_tensors_record_no_history():
     packed, w = mgd.mg_mx_pack(x), mgd.mg_mx_pack(x, "e2m1")
     for y in (packed.codes, mgd.mg_mx_unpack(packed), mgd.mg_mx4_linear(x, w), *mgd.mg_mx8_weight_gradient(x, packed)):
         assert not y.requires_grad
+
+
+@pytest.mark.parametrize("dtype", DTYPES)
+@pytest.mark.parametrize("T", [7, 28, 100])
+def test_infinite_gradients_among_many_rows(dtype, T):
+    """Over many workgroups: channels without one keep the bits they have without any, rows past the counts none."""
+    t, inf = DTYPES[dtype], float("inf")
+    gen = torch.Generator("cuda").manual_seed(T)
+    B, N, E = 6, 2040, 256
+    x = torch.randn((B, N, E), device="cuda", generator=gen).abs() + 0.5
+    g = torch.randn((B, N, T), device="cuda", generator=gen).to(t)
+    natoms = torch.tensor([2040, 1000, 0, 33, 2040, 7], dtype=torch.int32, device="cuda")
+    packed = mgd.mg_mx_pack(x)
+    clean = mgd.mg_mx8_weight_gradient(g, packed, natoms=natoms)
+    g[1, 1000:], g[2], g[5, 7] = inf, float("nan"), -inf            # of no atom
+    for a, b in zip(mgd.mg_mx8_weight_gradient(g, packed, natoms=natoms), clean):
+        assert torch.equal(a, b)
+    g[0, 2039, 3], g[4, 5, 3], g[1, 999, 5], g[4, 0, 6], g[3, 32, 6] = inf, inf, -inf, inf, -inf
+    dw, db = mgd.mg_mx8_weight_gradient(g, packed, natoms=natoms)
+    assert (dw[3] == inf).all() and (dw[5] == -inf).all() and dw[6].isnan().all()
+    assert db[3] == inf and db[5] == -inf and db[6].isnan()
+    rest = [k for k in range(T) if k not in (3, 5, 6)]
+    assert torch.equal(dw[rest], clean[0][rest]) and torch.equal(db[rest], clean[1][rest])
