@@ -101,11 +101,11 @@ class _Exact:
 class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     """Within ``with saved_in_8_bits():`` what autograd saves for the backward pass is kept in 8 bits
     (blocks of 32 neighbouring numbers in memory that share a power of two) and restored when it is
-    needed.  Every save takes 33/32 bytes a number.  What several operations save (a ReLU's result is the next
-    convolution's input) is kept once for each of them, where torch holds it once: four convolutions
-    followed by ReLU take 0.41 of their float32 memory and 0.83 of bfloat16's, by softplus, where
-    nothing is saved twice, 0.26 and 0.52.  For the network behind a grid, whose activations are as
-    large as the grid:
+    needed.  Every save takes 33/32 bytes a number.  What several operations save (a ReLU's result is
+    the next convolution's input) is kept once for each of them, where torch holds it once: four
+    convolutions followed by ReLU take 0.41 of their float32 memory and 0.83 of bfloat16's, by softplus,
+    where nothing is saved twice, 0.26 and 0.52.  For the network behind a grid, whose activations are
+    as large as the grid:
 
         with saved_in_8_bits():
             loss = net(layer(coords, radii, types=types, T=T))
@@ -115,7 +115,8 @@ class saved_in_8_bits(torch.autograd.graph.saved_tensors_hooks):
     lie without gaps in memory, but for parameters (frozen ones too), other leaves that require a
     gradient, and views of either, which exist anyway, and the copies autocast makes of them in
     another type.  (Its copies of frozen weights cannot be told from data: have a frozen layer in the
-    type it runs in.)  Everything else, nested tensors and subclasses of tensors among it, and what this module's own layers save, stays exact.
+    type it runs in.)  Everything else, nested tensors and subclasses of tensors among it, and what
+    this module's own layers save, stays exact.
 
     ``format`` "int8" is off by at most 2^-7 of the block's largest number (256/255 of that where the
     largest is just below a power of two), "e4m3" by at most 2^-4 of each (or 1.2 times 2^-18 of the
@@ -278,8 +279,10 @@ class AtomTyper(torch.nn.Module):
     (``GridLayer(..., typer=AtomTyper(E, T))`` and ``layer(coords, radii, features=features)``).
 
     What the weight gradient needs of the features is kept in 8 bits (``keep`` "int8" or "e4m3") and
-    the gradient formed from the codes; ``keep=None`` leaves both to torch.  With ``natoms`` [B] (int32)
-    atoms past an example's count have no part in any gradient, whatever their rows hold.
+    the gradient formed from the codes, once: no second derivatives, forward mode or ``vmap``.  The map
+    itself and the features' gradient are torch's products; ``keep=None`` leaves all of it to torch.
+    With ``natoms`` [B] (int32) atoms past an example's count have no part in any gradient, whatever
+    their rows hold.
 
     A training step can be captured in a graph; as for every leaf in torch, no graph of the same
     parameters that was recorded outside may be alive at the capture (drop losses and outputs first).

@@ -21,9 +21,9 @@
 //   - The rows are split over workgroups and the eight wavefronts of each; partial sums are added in a
 //     fixed order (LDS, then a second kernel over the workgroups' sums), so the same call gives the same
 //     bits every time.
-// Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 16.6 us (38 MB: 2.3 TB/s; the
+// Measured (both kernels, back to back): 102000 x 256 int8, 28 channels of float 15.3 us (38 MB: 2.5 TB/s; the
 // first kernel 14, 3 to 4 steps a wavefront and their vector instructions, 5 a code); 96000 live of 128000 x
-// 1000 e4m3, 28 of bfloat16 28 us (110 MB: 3.9 TB/s); 512000 x 256 e4m3 32 us (5.1 TB/s).
+// 1000 e4m3, 28 of bfloat16 27 us (110 MB: 4.1 TB/s); 512000 x 256 e4m3 29.5 us (5.6 TB/s).
 #include <type_traits>
 
 #include "mg_common.h"
@@ -263,8 +263,9 @@ __global__ __launch_bounds__(kThreads, 2) void gradient_kernel(GradientArgs a)
 done:
 
     // An infinity in a gradient of several pieces leaves NaN in the pieces after its first and makes its channel's
-    // sums NaN in every column.  A wavefront that finds one walks its rows once more, and there an infinity is whole in its
-    // first piece.  (Looked for in the walk above: 15.3 -> 15.7 us at 102000 x 256 x 28, 22.6 -> 23.6 at 32640 x 512 x 100.)
+    // sums NaN in every column.  A wavefront that finds one walks its rows once more, and there an infinity is whole
+    // in its first piece.  (Looked for in the walk above it costs 15.4 -> 15.7 us at 102000 x 256 x 28 floats and
+    // 22.9 -> 23.6 at 32640 x 512 x 100; without either 15.4 and 22.6.)
     if constexpr (kPieces<T> > 1) {
         float any = 0.0f;
 #pragma unroll

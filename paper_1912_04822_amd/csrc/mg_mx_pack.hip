@@ -5,9 +5,9 @@
 // the plain numbers and the codes are moved in runs that are contiguous over the wavefront.  Magnitudes
 // are compared as unsigned words, where a NaN is larger than everything: a block that is not finite is
 // found by its maximum alone.  Both directions are bound by memory: a number is read or written once and
-// meets about a dozen instructions.  Measured, with a copy at 5.1 TB/s (read and written): 155 million floats
-// to int8 in 119 us and back in 110 (6.6 and 7.1 TB/s of their 0.78 GB), 22 million bfloat16 to e4m3 and back
-// in 13 each (5.1), 128000 odd rows of 509 halves to e2m1 in 37 (4.5) and back in 28.
+// meets about a dozen instructions.  Measured (medians of launches), with a copy at 5.1 TB/s (read and written):
+// 155 million floats to int8 in 127 us and back in 99 (6.1 and 7.8 TB/s of their 0.78 GB), 22 million bfloat16
+// to e4m3 in 12.8 and back in 12.4 (5.3), 128000 odd rows of 509 halves to e2m1 in 44 (3.8) and back in 26.5 (6.2).
 #include "mg_common.h"
 #include "mg_mx.h"
 
