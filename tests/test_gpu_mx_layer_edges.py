@@ -222,3 +222,36 @@ def test_nested_tensors_and_subclasses_are_saved_as_they_are():
         (y.to_padded_tensor(0.0) if x.is_nested else y).sum().backward()
         got, want = (x.grad.to_padded_tensor(0.0), x.detach().to_padded_tensor(0.0)) if x.is_nested else (x.grad, x.detach())
         assert torch.equal(got, 2 * want)
+
+
+@pytest.mark.parametrize("keep", ["int8", "e4m3"])
+def test_types_under_autocast(keep):
+    """The map runs in bfloat16, what is kept comes from the features as they are: the weight's and bias's
+    gradients are those outside, to the bit."""
+    torch.manual_seed(7)
+    typer = AtomTyper(70, 9, keep=keep).cuda()
+    x = torch.randn((3, 200, 70), device="cuda", requires_grad=True)
+    natoms = torch.tensor([200, 0, 77], dtype=torch.int32, device="cuda")
+    G = torch.randn((3, 200, 9), device="cuda")
+    leaves = [x, typer.weight, typer.bias]
+    want = torch.autograd.grad(typer(x, natoms), leaves, G)
+    with torch.autocast("cuda", dtype=torch.bfloat16):
+        y = typer(x, natoms)
+        low = torch.nn.functional.linear(x, typer.weight, typer.bias)
+    assert y.dtype == torch.float32 and low.dtype == torch.bfloat16 and torch.equal(y, low.float())
+    got = torch.autograd.grad(y, leaves, G)
+    for a, b in zip(got, want):
+        assert a.dtype == torch.float32 and torch.equal(a, b)
+
+
+def test_several_steps_alive_at_once_and_out_of_order():
+    """Two forward passes before either backward pass, taken in the other order, one of them twice."""
+    torch.manual_seed(8)
+    typer = AtomTyper(40, 5).cuda()
+    xs = [torch.randn((2, 60, 40), device="cuda") for _ in range(2)]
+    Gs = [torch.randn((2, 60, 5), device="cuda") for _ in range(2)]
+    want = [torch.autograd.grad(typer(x), list(typer.parameters()), G) for x, G in zip(xs, Gs)]
+    ys = [typer(x) for x in xs]
+    for k in (1, 0, 1):
+        for a, b in zip(torch.autograd.grad(ys[k], list(typer.parameters()), Gs[k], retain_graph=True), want[k]):
+            assert torch.equal(a, b)
